@@ -62,8 +62,11 @@ typedef enum {
     ICONV_U8 = 0,        /* unsigned 8-bit activation */
     ICONV_S8 = 1,        /* signed 8-bit activation */
     ICONV_I32 = 2,       /* raw int32 Y (projection skips, logits) */
-    ICONV_U8_RAW128 = 3  /* raw uint8 image; 128 is subtracted on load (Section 3.4.1).
+    ICONV_U8_RAW128 = 3, /* raw uint8 image; 128 is subtracted on load (Section 3.4.1).
                             Padding is zero AFTER the subtraction. */
+    ICONV_F32 = 4,       /* floating rows: irms_quant and imat_forward only */
+    ICONV_F16 = 5,
+    ICONV_BF16 = 6
 } iconv_dtype;
 
 /* Kernel families; ICONV_KERNEL_AUTO lets the plan choose. */
@@ -319,6 +322,88 @@ typedef struct {
 } istem_desc;
 ICONV_API int iconv_stem_forward_static(const istem_desc *desc, const void *x, const int8_t *weights, const int32_t *bias,
                               void *out, void *cuda_stream);
+
+/*
+ * ---- The feed-forward sublayer of a transformer in 8 bits (the paper has no counterpart; its numerics do: symmetric int8 with a
+ * scale, Section 3.1, int32 sums).  A row is one token.  A matrix of rows is given by its address and its row stride in ELEMENTS; what
+ * lies between a row's end and the next row is neither read nor written.
+ *
+ * irms_quant -- the residual's addition, the root-mean-square norm and 8-bit rows with a scale each:
+ *     s = x + residual                         in float
+ *     sum = s                                  rounded to dtype
+ *     v = s * weight                           in float
+ *     q = [127 * v / max|v|]                   the bracket of Eq. 4: v * (127 / max|v|) in float, then floor(. + 1/2); -127 ... 127
+ *     scales[row] = max|v| / 127 / sqrt(mean(s^2) + eps)
+ * q * scale stands for the normed row (the root cancels in q: rounding never depends on it).  norm = 0: the 8-bit rows alone,
+ * scales[row] = max|v| / 127.  A row whose max|v| is zero, or lies under 2^-119, has q = 0 and scale 0; one with a NaN or an infinity in
+ * v has q = 0 and scale NaN.
+ *   x, residual   DEVICE rows x width of dtype (ICONV_F32, ICONV_F16 or ICONV_BF16); residual NULL: none
+ *   weight        DEVICE [width] of weight_dtype (dtype or ICONV_F32); NULL: ones
+ *   sum           DEVICE rows x width of dtype, or NULL: not written; may be x or residual itself, at the same stride
+ *   q             DEVICE int8 rows x width; scales DEVICE float [rows]
+ * Addresses are aligned to their element (16-byte aligned ones and strides in multiples of 16 bytes -- 8 for q, 4 with ICONV_F32 -- are
+ * the fast form).  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t width;
+    int32_t dtype, weight_dtype;
+    int32_t norm;                      /* 1: root-mean-square norm; 0: 8-bit rows of the sum as it is */
+    float eps;                         /* >= 0 */
+    int64_t x_stride, residual_stride, sum_stride, q_stride;   /* elements, >= width (those of NULL matrices are ignored) */
+} irms_desc;
+ICONV_API int irms_quant(const irms_desc *desc, const void *x, const void *residual, const void *weight, void *sum, int8_t *q,
+                         float *scales, void *cuda_stream);
+
+/*
+ * imat_plan / imat_forward -- 8-bit rows times int8 weights (int32 sums on the tensor cores, exact), with everything behind the sums in
+ * the same kernel:
+ *     acc[m][c] = sum_k x[m][k] * weights[c][k]
+ *     y = act(acc * x_scales[m] * scales[c] + bias[c])
+ *     out[m][c] = y + residual[m][c]                            rounded to out_dtype (float until then)
+ * and, with up_weights, both projections of a gated feed-forward block in one kernel:
+ *     out[m][c] = act(gate) * up,   gate = acc * x_scales[m] * scales[c] + bias[c],   up = the same of up_weights, up_scales, up_bias
+ * With irms_quant before them these make the sublayer: norm -> gated product -> 8-bit rows -> product with the residual.
+ *
+ * imat_plan copies the weights into a layout of its own, n * k bytes (twice that when gated) rounded up to blocks of 128 x 128, with
+ * cudaMalloc on the current device; what desc points to may go afterwards.  It enqueues on cuda_stream and waits for it: call it outside any
+ * stream capture, on the stream that wrote the weights.  ICONV_ERR_OVERFLOW when k reaches 131072 (the sums would not fit
+ * int32 whatever the values).
+ * imat_forward: a plan belongs to its device, which must be current.  It enqueues one kernel, needs no workspace and keeps nothing: calls of
+ * one plan may overlap on any streams and may be captured.
+ *   x          DEVICE int8 rows x k, 16-byte aligned, x_stride a multiple of 16 (k itself may be anything)
+ *   x_scales   DEVICE float [rows], 16-byte aligned
+ *   residual   DEVICE rows x n of out_dtype, or NULL; may be out itself at the same stride.  Not with a gated plan (ICONV_ERR_UNSUPPORTED)
+ *   out        DEVICE rows x n of out_dtype; out and residual are aligned to their element
+ * Results do not depend on the number of rows in the call.  NaN and infinities in the scales, the bias and the residual come out as the
+ * formula gives them.  rows = 0 is a no-op; at most 2^30 rows.
+ */
+typedef enum {
+    IMAT_NONE = 0,
+    IMAT_RELU = 1,
+    IMAT_SILU = 2,         /* y / (1 + exp(-y)) */
+    IMAT_GELU = 3,         /* y / 2 * (1 + erf(y / sqrt 2)) */
+    IMAT_GELU_TANH = 4     /* y / 2 * (1 + tanh(sqrt(2 / pi) * (y + 0.044715 y^3))) */
+} imat_act;
+typedef struct {
+    int32_t n, k;                      /* output channels, length of the reduction */
+    int32_t out_dtype;                 /* ICONV_F32 | ICONV_F16 | ICONV_BF16 */
+    int32_t act;                       /* imat_act */
+    const int8_t *weights;             /* device [n][k], rows w_stride apart */
+    int64_t w_stride;                  /* >= k; any */
+    const float *scales;               /* device [n] */
+    const float *bias;                 /* device [n], or NULL */
+    const int8_t *up_weights;          /* device, as weights; NULL: not gated */
+    const float *up_scales;            /* device [n] (with up_weights) */
+    const float *up_bias;              /* device [n], or NULL */
+} imat_desc;
+typedef struct imat_plan_s imat_plan_t;
+ICONV_API int imat_plan(const imat_desc *desc, void *cuda_stream, imat_plan_t **plan_out);
+ICONV_API int imat_plan_destroy(imat_plan_t *plan);
+ICONV_API int imat_forward(const imat_plan_t *plan, int64_t rows, const int8_t *x, int64_t x_stride, const float *x_scales,
+                           const void *residual, int64_t residual_stride, void *out, int64_t out_stride, void *cuda_stream);
+/* One line of text on how a call of `rows` rows runs (kernel, tile, split), as iconv_plan_describe. */
+ICONV_API int imat_plan_describe(const imat_plan_t *plan, int64_t rows, char *text, size_t size);
 
 /* ---- host-side parameter arithmetic (no GPU involved) ------------------------------- */
 

@@ -11,9 +11,11 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libiconv_b200.so")
 
 OK, ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_OVERFLOW, ERR_UNSUPPORTED, ERR_CUDA, ERR_TIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
-U8, S8, I32, U8_RAW128 = 0, 1, 2, 3
+U8, S8, I32, U8_RAW128, F32, F16, BF16 = 0, 1, 2, 3, 4, 5, 6
 KERNEL_AUTO, KERNEL_DIRECT, KERNEL_UMMA, KERNEL_THIN, KERNEL_STEM, KERNEL_UMMA_IM2COL = 0, 1, 2, 3, 4, 5
-DTYPE_CODE = {"u8": U8, "s8": S8, "i32": I32, "u8_raw128": U8_RAW128}
+DTYPE_CODE = {"u8": U8, "s8": S8, "i32": I32, "u8_raw128": U8_RAW128, "f32": F32, "f16": F16, "bf16": BF16}
+IMAT_NONE, IMAT_RELU, IMAT_SILU, IMAT_GELU, IMAT_GELU_TANH = 0, 1, 2, 3, 4
+ACT_CODE = {"none": IMAT_NONE, "relu": IMAT_RELU, "silu": IMAT_SILU, "gelu": IMAT_GELU, "gelu_tanh": IMAT_GELU_TANH}
 KERNEL_NAME = {KERNEL_DIRECT: "direct", KERNEL_UMMA: "umma", KERNEL_THIN: "thin", KERNEL_STEM: "stem"}
 
 EXPORTS = ("iconv_plan", "iconv_plan_stem_pool", "iconv_plan_destroy", "iconv_plan_kernel", "iconv_plan_describe", "iconv_workspace_bytes", "iconv_forward",
@@ -21,7 +23,8 @@ EXPORTS = ("iconv_plan", "iconv_plan_stem_pool", "iconv_plan_destroy", "iconv_pl
            "iconv_forward_chain", "iconv_plan_stack", "iconv_stack_destroy", "iconv_stack_sync_bytes", "iconv_forward_stack",
            "iadd_requant", "ipool_max", "ipool_avg_requant", "iq_weight_delta", "iq_quantize_weights",
            "iq_mul_shift", "iq_brelu_params", "iq_skip_sync", "iq_sigma_bound", "iq_release_scratch", "iq_bn_fold", "iconcat_plan",
-           "iconv_stem_forward_static", "iconv_last_error")
+           "iconv_stem_forward_static", "irms_quant", "imat_plan", "imat_plan_destroy", "imat_forward",
+           "imat_plan_describe", "iconv_last_error")
 
 
 class IconvError(RuntimeError):
@@ -57,6 +60,16 @@ class istem_desc(C.Structure):
     _fields_ = [(k, C.c_int32) for k in (
         "n", "h", "w", "c_out", "in_dtype", "out_c_total", "out_c_offset", "mul", "shift", "h_i",
         "out_lo", "out_hi", "out_zero")]
+
+
+class irms_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64)] + [(k, C.c_int32) for k in ("width", "dtype", "weight_dtype", "norm")] + [("eps", C.c_float)] + [
+        (k, C.c_int64) for k in ("x_stride", "residual_stride", "sum_stride", "q_stride")]
+
+
+class imat_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("n", "k", "out_dtype", "act")] + [("weights", C.c_void_p), ("w_stride", C.c_int64)] + [
+        (k, C.c_void_p) for k in ("scales", "bias", "up_weights", "up_scales", "up_bias")]
 
 
 STEM_STATIC_BYTES = 32 * 1024 * 1024
@@ -100,6 +113,11 @@ def _load():
     lib.iq_bn_fold.argtypes = [vp, vp, vp, vp, vp, vp, dbl, i32, i64, vp, vp, vp]
     lib.iconcat_plan.argtypes = [i32, vp, vp, i32, vp, vp, vp, vp, P(dbl)]
     lib.iconv_stem_forward_static.argtypes = [P(istem_desc), vp, vp, vp, vp, vp]
+    lib.irms_quant.argtypes = [P(irms_desc), vp, vp, vp, vp, vp, vp, vp]
+    lib.imat_plan.argtypes = [P(imat_desc), vp, P(vp)]
+    lib.imat_plan_destroy.argtypes = [vp]
+    lib.imat_forward.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp]
+    lib.imat_plan_describe.argtypes = [vp, i64, C.c_char_p, C.c_size_t]
     lib.iconv_last_error.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("iconv_last_error", "iconv_workspace_bytes", "iconv_stack_sync_bytes"):
@@ -362,3 +380,37 @@ def iconv_stem_forward_static(x_ptr, weights_ptr, bias_ptr, out_ptr, stream=0, *
                    out_c_total=c_out if out_c_total is None else out_c_total, out_c_offset=out_c_offset,
                    mul=int(mul), shift=int(shift), h_i=int(h_i), out_lo=out_lo, out_hi=out_hi, out_zero=out_zero)
     _check(lib.iconv_stem_forward_static(C.byref(d), x_ptr, weights_ptr, bias_ptr, out_ptr, stream))
+
+
+def irms_quant(x_ptr, residual_ptr, weight_ptr, sum_ptr, q_ptr, scales_ptr, stream=0, *, rows, width, dtype, weight_dtype=None, eps=0.0, norm=1,
+               x_stride=None, residual_stride=None, sum_stride=None, q_stride=None):
+    """Residual addition, root-mean-square norm and 8-bit rows with a scale each; strides in elements (default: dense rows)."""
+    dense = lambda s: width if s is None else s
+    d = irms_desc(rows=rows, width=width, dtype=dtype, weight_dtype=dtype if weight_dtype is None else weight_dtype, norm=norm, eps=eps,
+                  x_stride=dense(x_stride), residual_stride=dense(residual_stride), sum_stride=dense(sum_stride), q_stride=dense(q_stride))
+    _check(lib.irms_quant(C.byref(d), x_ptr, residual_ptr, weight_ptr, sum_ptr, q_ptr, scales_ptr, stream))
+
+
+def imat_plan(*, n, k, out_dtype, act=IMAT_NONE, weights, scales, bias=None, up_weights=None, up_scales=None, up_bias=None, w_stride=None, stream=0):
+    """Plan a product with int8 weights [n][k] (or, with ``up_weights``, both projections of a gated block); returns an opaque handle
+    (int).  All pointers are DEVICE addresses; the weights are copied."""
+    d = imat_desc(n=n, k=k, out_dtype=out_dtype, act=act, weights=weights, w_stride=k if w_stride is None else w_stride, scales=scales, bias=bias,
+                  up_weights=up_weights, up_scales=up_scales, up_bias=up_bias)
+    plan = C.c_void_p()
+    _check(lib.imat_plan(C.byref(d), stream, C.byref(plan)))
+    return plan.value
+
+
+def imat_plan_destroy(plan):
+    _check(lib.imat_plan_destroy(plan))
+
+
+def imat_forward(plan, rows, x_ptr, x_stride, x_scales_ptr, residual_ptr, residual_stride, out_ptr, out_stride, stream=0):
+    """One product of ``rows`` 8-bit rows; strides in elements."""
+    _check(lib.imat_forward(plan, rows, x_ptr, x_stride, x_scales_ptr, residual_ptr, residual_stride, out_ptr, out_stride, stream))
+
+
+def imat_plan_describe(plan, rows) -> str:
+    buf = C.create_string_buffer(256)
+    _check(lib.imat_plan_describe(plan, rows, buf, 256))
+    return buf.value.decode()

@@ -13,8 +13,9 @@ OBJ_DIR = os.path.join(_HERE, "_build")
 PROBE_SRC = os.path.join(_HERE, "bench_probe", "probe_mma.cu")
 PROBE_LIB = os.path.join(_HERE, "libiconv_probe.so")
 SOURCES = ["iconv_api.cu", "plan.cu", "kernels_direct.cu", "kernel_thin.cu", "kernel_umma.cu", "kernel_stem.cu",
-           "kernel_calib.cu", "kernel_chain.cu", "kernel_stack.cu", "kernel_picture.cu", "kernel_pool.cu", "kernel_flow.cu", "planner.cpp"] + ["umma_inst_conv%d.cu" % e for e in range(8)] + \
-          ["umma_inst_window%d.cu" % e for e in (2, 3, 4, 5, 8)] + ["umma_inst_roll%d.cu" % e for e in (2, 4, 8)]
+           "kernel_calib.cu", "kernel_chain.cu", "kernel_stack.cu", "kernel_picture.cu", "kernel_pool.cu", "kernel_flow.cu", "kernel_rms.cu", "kernel_mat.cu",
+           "planner.cpp"] + ["umma_inst_conv%d.cu" % e for e in range(8)] + \
+          ["umma_inst_window%d.cu" % e for e in (2, 3, 4, 5, 8)] + ["umma_inst_roll%d.cu" % e for e in (2, 4, 8)] + ["mat_inst%d.cu" % e for e in range(3)]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-diag-suppress", "128", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-fvisibility=hidden", "-I", INCLUDE, "-I", CSRC]
 
@@ -49,7 +50,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         src, obj = os.path.join(CSRC, s), os.path.join(OBJ_DIR, s + ".o")
         if force or _stale(obj, [src] + headers):
             jobs.append((src, obj))
-    jobs.sort(key=lambda j: -os.path.getsize(j[0]) if "umma_inst" not in j[0] else -10 ** 9)   # the kernel instances first: they take longest
+    jobs.sort(key=lambda j: -os.path.getsize(j[0]) if "_inst" not in j[0] else -10 ** 9)   # the kernel instances first: they take longest
     with ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 1))) as ex:
         for f in [ex.submit(_compile, src, obj, verbose) for src, obj in jobs]:
             f.result()

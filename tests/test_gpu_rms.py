@@ -1,0 +1,155 @@
+"""``irms_quant`` against its definition in 64 bits."""
+import pytest
+import torch
+
+from ff_util import TYPES, generator, ptr, rms_call, rms_check, stream
+from paper_2006_11735_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def _data(seed, m, d, dtype, residual=True, weight="same", pad=0):
+    gen = generator(seed)
+    rnd = lambda: torch.randn(m, d + pad, generator=gen, device="cuda").to(TYPES[dtype])[:, :d]
+    x, r = rnd(), 2 * rnd() if residual else None
+    g = None if weight is None else (1 + 0.3 * torch.randn(d, generator=gen, device="cuda")).to(TYPES[dtype] if weight == "same" else torch.float32)
+    return x, r, g
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [1, 7, 8, 64, 255, 256, 257, 513, 1000, 1024, 2048, 2056, 4096, 4100, 8192, 16384, 16392, 32768, 32776, 40001])
+def test_widths(dtype, d):
+    """Every instance of the kernel: rows in a warp, in a block, in registers and read twice; whole vectors and single elements."""
+    for m in (1, 5):
+        x, r, g = _data(d + m, m, d, dtype)
+        q, scales, total = rms_call(x, r, g)
+        rms_check(x, r, g, q, scales, total)
+    B.iconv_check(stream())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("weight", [None, "same", "f32"])
+@pytest.mark.parametrize("norm", [0, 1])
+def test_forms(dtype, residual, weight, norm):
+    for d in (520, 521):
+        x, r, g = _data(3, 33, d, dtype, residual, weight)
+        for with_sum in (True, False):
+            q, scales, total = rms_call(x, r, g, norm=norm, with_sum=with_sum)
+            rms_check(x, r, g, q, scales, total, norm=norm)
+
+
+@pytest.mark.parametrize("pad", [1, 8])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_strides_leave_what_is_between_rows(pad, dtype):
+    m, d = 19, 1024
+    x, r, g = _data(5, m, d, dtype, pad=pad)
+    q_store = torch.full((m + 1, d + 16), 77, dtype=torch.int8, device="cuda")
+    sum_store = torch.full((m + 1, d + pad), 9, dtype=TYPES[dtype], device="cuda")
+    scales = torch.full((m + 3,), 5.0, device="cuda")
+    q, total = q_store[:m, :d], sum_store[:m, :d]
+    rms_call(x, r, g, q=q, total=total, scales=scales)
+    rms_check(x, r, g, q, scales[:m], total)
+    assert (q_store[:, d:] == 77).all() and (q_store[m] == 77).all() and (sum_store[:, d:] == 9).all() and (sum_store[m] == 9).all()
+    assert (scales[m:] == 5).all()
+
+
+@pytest.mark.parametrize("d", [512, 513, 40000])
+@pytest.mark.parametrize("into", ["x", "r"])
+def test_sum_in_place(d, into):
+    x, r, g = _data(7, 6, d, "bf16")
+    want = rms_call(x, r, g)
+    x2, r2 = x.clone(), r.clone()
+    q, scales, total = rms_call(x2, r2, g, total=x2 if into == "x" else r2)
+    assert torch.equal(q, want[0]) and torch.equal(scales, want[1]) and torch.equal(total, want[2])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_of_zeros_and_tiny_rows(dtype):
+    x = torch.zeros(6, 300, dtype=TYPES[dtype], device="cuda")
+    x[1, 5] = torch.finfo(TYPES[dtype]).tiny
+    x[3] = 1.0
+    if dtype != "f16":
+        x[4, 7] = 2.0 ** -119
+        x[5, 7] = 2.0 ** -120
+    q, scales, total = rms_call(x)
+    rms_check(x, None, None, q, scales, total)
+    assert scales[0] == 0 and (q[0] == 0).all() and (q[3] == 127).all() and torch.equal(total, x)
+    if dtype != "f16":
+        assert q[4, 7] == 127 and q[5, 7] == 0
+    q, scales, _ = rms_call(x[:1], eps=0.0)                 # nothing to divide by: still nothing
+    assert scales[0] == 0 and (q == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 700, 40000])
+def test_squares_that_do_not_fit(dtype, d):
+    x = torch.randn(4, d, generator=generator(1), device="cuda") * torch.tensor([1e19, 1e25, 1e30, 3e37], device="cuda")[:, None]
+    x = x.clamp(-3e38, 3e38).to(TYPES[dtype])
+    q, scales, total = rms_call(x)
+    rms_check(x, None, None, q, scales, total)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [96, 1024, 1025, 40000])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_bad_value_spoils_its_row_alone(dtype, d, bad):
+    x, r, g = _data(9, 5, d, dtype)
+    clean = rms_call(x, r, g)
+    x[2, d - 1] = bad
+    for norm in (0, 1):
+        q, scales, total = rms_call(x, r, g, norm=norm)
+        assert torch.isnan(scales[2]) and (q[2] == 0).all()
+        keep = [0, 1, 3, 4]
+        assert torch.equal(q[keep], clean[0][keep]) and torch.isfinite(scales[keep]).all()
+        assert torch.equal(total[keep], clean[2][keep])
+
+
+def test_infinite_weight_and_infinities_that_cancel():
+    x, r, g = _data(2, 3, 64, "f32")
+    x[1, 3], r[1, 3] = float("inf"), float("-inf")          # NaN
+    q, scales, _ = rms_call(x, r, g)
+    assert torch.isnan(scales[1]) and not torch.isnan(scales[[0, 2]]).any()
+    g[5] = float("inf")
+    q, scales, _ = rms_call(x, r, g)
+    assert torch.isnan(scales).all() and (q == 0).all()
+
+
+def test_many_rows_and_offsets_past_32_bits():
+    m, d = 70001, 96
+    x, r, g = _data(4, m, d, "bf16")
+    rms_check(x, r, g, *rms_call(x, r, g))
+    far = torch.zeros(3, 1 << 30, dtype=torch.bfloat16, device="cuda")          # the last row starts 4 GB behind the first
+    x = far[:, :d]
+    x.copy_(torch.randn(3, d, generator=generator(6), device="cuda"))
+    rms_check(x, None, None, *rms_call(x, with_sum=False), eps=1e-5)
+
+
+def test_same_rows_in_another_call():
+    x, r, g = _data(8, 40, 4096, "bf16")
+    q, scales, total = rms_call(x, r, g)
+    for i in (0, 17, 39):
+        a, b, c = rms_call(x[i:i + 1], r[i:i + 1], g)
+        assert torch.equal(a, q[i:i + 1]) and torch.equal(b, scales[i:i + 1]) and torch.equal(c, total[i:i + 1])
+
+
+def test_captured_and_replayed_on_another_stream():
+    x, r, g = _data(10, 12, 2048, "f16")
+    q, scales, total = (torch.empty(12, 2048, dtype=torch.int8, device="cuda"), torch.empty(12, device="cuda"), torch.empty_like(x))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        rms_call(x, r, g, q=q, total=total, scales=scales)
+        with torch.cuda.graph(graph, stream=side):
+            rms_call(x, r, g, q=q, total=total, scales=scales)
+    x.copy_(torch.randn(12, 2048, generator=generator(11), device="cuda"))
+    graph.replay()
+    torch.cuda.synchronize()
+    rms_check(x, r, g, q, scales, total)
+
+
+def test_no_rows():
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    B.irms_quant(None, None, None, None, None, None, stream(), rows=0, width=64, dtype=B.BF16)
+    assert rms_call(x)[0].shape == (0, 64) and ptr(x) is not None
