@@ -250,7 +250,8 @@ cudaError_t launch_one(const RmsArgs &a, cudaStream_t stream)
 {
     constexpr int ROWS = TPR > 128 ? 1 : 128 / TPR;
     const long long blocks = (a.rows + ROWS - 1) / ROWS;
-    return launch_kernel(rms_quant_kernel<T, VE, TPR, R>, true, (unsigned)blocks, TPR > 128 ? TPR : 128, 0, stream, a);
+    const auto kernel = rms_quant_kernel<T, VE, TPR, R>;
+    return launch_kernel(kernel, true, (unsigned)blocks, TPR > 128 ? TPR : 128, 0, stream, a);
 }
 
 template <typename T, int VE>

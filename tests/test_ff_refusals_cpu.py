@@ -1,7 +1,12 @@
-"""What ``irms_quant`` and ``imat_plan`` refuse, before anything touches a GPU (addresses are never read here)."""
+"""What ``irms_quant`` and ``imat_plan`` refuse, before anything touches a GPU (addresses are never read here), and how their kernels, which
+come up while the kernel before them still runs, read their tensors."""
+import os
+import re
+
 import pytest
 
 from paper_2006_11735_b200 import binding as B
+from paper_2006_11735_b200.build import CSRC
 
 A = 1 << 20         # a well-aligned address that nothing reads
 
@@ -48,3 +53,11 @@ def test_plan_refuses(kw, status):
 
 def test_no_rows_need_no_memory():
     _rms(x=None, q=None, scales=None, rows=0)
+
+
+@pytest.mark.parametrize("file", ["kernel_rms.cu", "mat_device.cuh"])
+def test_tensors_are_read_by_plain_loads(file):
+    """The read-only path is for the plan's constants alone."""
+    text = open(os.path.join(CSRC, file)).read()
+    assert "__restrict__" not in text and not re.search(r"\.nc\b", text) and "grid_dep_wait()" in text
+    assert all(m.group(1).startswith("a.row_params") for m in re.finditer(r"__ldg\((.*)", text))
