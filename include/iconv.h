@@ -341,8 +341,8 @@ ICONV_API int iconv_stem_forward_static(const istem_desc *desc, const void *x, c
  *   weight        DEVICE [width] of weight_dtype (dtype or ICONV_F32); NULL: ones
  *   sum           DEVICE rows x width of dtype, or NULL: not written; may be x or residual itself, at the same stride
  *   q             DEVICE int8 rows x width; scales DEVICE float [rows]
- * Addresses are aligned to their element (16-byte aligned ones and strides in multiples of 16 bytes -- 8 for q, 4 with ICONV_F32 -- are
- * the fast form).  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
+ * Addresses are aligned to their element (16-byte aligned ones, and a width and strides in multiples of 16 bytes -- 8
+ * for q, 4 with ICONV_F32 -- are the fast form).  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
  */
 typedef struct {
     int64_t rows;

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -26,8 +27,10 @@ constexpr int MAT_K_MAX = 131071;          // 128 * 128 * k stays under 2^31
 
 // What one call runs.
 struct MatChoice {
-    int split;                             // 0: bulk kernel
-    int nt, tok_tiles, stages, stage_bytes, tmem_cols;
+    bool streams, bulk;                    // the streaming kernel, the bulk kernel, else the few-tile kernel
+    int warps;                             // of a block of the streaming kernel
+    int split;                             // parts of a tile's reduction
+    int nt, tok_tiles, stages, stage_bytes, recv_bytes, tmem_cols;
     unsigned grid;
     size_t smem;
 };
@@ -85,54 +88,122 @@ __global__ void __launch_bounds__(256) mat_pack_kernel(const __grid_constant__ P
 
 int round_up(int v, int to) { return (v + to - 1) / to * to; }
 
-void stages_of(MatChoice &c, int room, int k_blocks)
-{
-    c.stages = std::min(std::min(room / c.stage_bytes, MAT_STAGES_MAX), std::max(k_blocks, 2));
-    c.smem = 1024 + (size_t)c.stages * c.stage_bytes + sizeof(MatShared);
-}
-
 constexpr int MAT_ROOM = MAX_SMEM - 1024 - (int)sizeof(MatShared);
+constexpr int MAT_ROOM_HALF = MAX_SMEM / 2 - 1024 - 1024 - (int)sizeof(MatShared);      // two blocks on an SM (each takes 1 KB of the system's besides)
 
-MatChoice choose_few(const imat_plan_t *p, long long rows)
+// Everything of a choice that follows from kernel, split and tokens of a tile.
+MatChoice choice(const imat_plan_t *p, long long rows, bool bulk, int split, int nt)
 {
     MatChoice c;
-    c.tok_tiles = (int)((rows + 127) / 128);
-    c.nt = round_up((int)((rows + c.tok_tiles - 1) / c.tok_tiles), 16);
-    c.stage_bytes = MAT_BLOCK + c.nt * 128;
-    c.tmem_cols = 32;
-    while (c.tmem_cols < c.nt) c.tmem_cols *= 2;
-    const long long tiles = (long long)p->ch_tiles * c.tok_tiles;
-    c.split = 1;
-    while (c.split < 8 && tiles * c.split * 2 <= p->sms + p->sms / 8 && p->k_blocks >= 4 * c.split) c.split *= 2;
-    c.grid = (unsigned)(tiles * c.split);
-    stages_of(c, MAT_ROOM, (p->k_blocks + c.split - 1) / c.split);
-    const size_t parts = 1024 + (size_t)c.nt * BLOCK_M * 4 + sizeof(MatShared);      // a split tile's sums lie where the stages were
-    while (c.split > 1 && c.smem < parts) { ++c.stages; c.smem += c.stage_bytes; }
+    c.streams = false; c.warps = 0;
+    c.bulk = bulk; c.split = split; c.nt = nt;
+    c.tok_tiles = (int)((rows + nt - 1) / nt);
+    c.stage_bytes = MAT_BLOCK + (bulk ? nt / 2 : nt) * 128;
+    c.recv_bytes = split > 1 ? (split - 1) * ((nt / MAT_PIECE + split - 1) / split) * MAT_PIECE_BYTES : 0;
+    c.tmem_cols = bulk ? 2 * MAT_BULK_TOKENS : 32;
+    while (c.tmem_cols < nt) c.tmem_cols *= 2;
+    const long long tiles = (long long)(bulk ? (p->ch_tiles + 1) / 2 : p->ch_tiles) * c.tok_tiles;
+    c.grid = bulk ? 2u * (unsigned)std::min<long long>(tiles, p->sms / 2) : (unsigned)(tiles * split);
+    const int blocks = bulk ? MAT_STAGES_MAX : (p->k_blocks + split - 1) / split;
+    const int room = bulk || c.grid <= (unsigned)p->sms ? MAT_ROOM : MAT_ROOM_HALF;
+    c.stages = std::max(2, std::min(std::min((room - c.recv_bytes) / c.stage_bytes, MAT_STAGES_MAX), blocks));
+    c.smem = 1024 + (size_t)c.stages * c.stage_bytes + c.recv_bytes + sizeof(MatShared);
     return c;
 }
 
-MatChoice choose_bulk(const imat_plan_t *p, long long rows)
+// Few tiles take sixteen warps each to keep the memory busy, many take four, several of them on an SM.
+MatChoice choice_stream(const imat_plan_t *p, long long rows)
 {
-    MatChoice c;
-    c.split = 0;
-    const long long pairs = p->sms / 2, ch_pairs = (p->ch_tiles + 1) / 2;
-    long long best = -1;
-    for (int nt = 256; nt >= 64; nt -= 32) {
-        const long long tok_tiles = (rows + nt - 1) / nt, rounds = (ch_pairs * tok_tiles + pairs - 1) / pairs;
-        const long long cost = rounds * (nt + 16);
-        if (best < 0 || cost < best) { best = cost; c.nt = nt; c.tok_tiles = (int)tok_tiles; }
+    MatChoice c = {};
+    c.streams = true;
+    const int blocks = p->gated ? (p->n + 15) / 16 : (p->n + 31) / 32, warps = blocks <= p->sms ? 16 : blocks <= 2 * p->sms ? 8 : 4;
+    c.warps = warps; c.split = 1;
+    c.nt = (int)rows; c.tok_tiles = 1;
+    c.grid = (unsigned)(p->gated ? (p->n + 15) / 16 : (p->n + 31) / 32);
+    c.smem = (size_t)warps * (rows > 8 ? 16 : 8) * MAT_STREAM_PITCH * 4;
+    return c;
+}
+
+// Which kernel, tile and split a call runs: the least of a time estimate over what there is.  The estimate is in nanoseconds and follows what bounds each
+// form on a B200 as measured: a block's way from L2 (87 bytes a nanosecond and SM, whatever the tile), its loads' latency (1100 ns for a round of
+// its stages), the issue of its instructions (190 ns for a block of 128 bytes of the reduction), HBM, then the epilogue.  It only has to rank the forms: over
+// 110 drawn sizes its choice took 3 % longer than the best of all forms on average (geometric mean), 33 % at most.
+constexpr double SM_RATE = 87.0, HBM_RATE = 6300.0, ROUND_LATENCY = 1100.0, ISSUE = 190.0;
+
+struct CallShape {
+    long long rows;
+    double weight_bytes, hbm;              // bytes of weights; nanoseconds that the call's bytes take from HBM
+    int residual, act;
+};
+
+CallShape shape_of(const imat_plan_t *p, long long rows, bool residual)
+{
+    CallShape s;
+    s.rows = rows;
+    s.weight_bytes = (double)p->n * p->k * (p->gated ? 2 : 1);
+    s.hbm = (s.weight_bytes + (double)rows * p->k + (double)rows * p->n * (p->out_dtype == ICONV_F32 ? 4 : 2) * (residual ? 2 : 1)) / HBM_RATE;
+    s.residual = residual; s.act = p->act != IMAT_NONE && p->act != IMAT_RELU;
+    return s;
+}
+
+// Few tokens, weights in registers: HBM at a rate that the tokens' own loads lower, or what an SM takes in.
+double cost_stream(const imat_plan_t *p, const CallShape &s, const MatChoice &c)
+{
+    const double from_hbm = s.weight_bytes / (5900.0 - 47.0 * (double)(s.rows - 1));
+    const double per_sm = (double)((c.grid + p->sms - 1) / p->sms) * MAT_STREAM_ROWS * 128.0 * p->k_blocks / (92.0 - 1.3 * (double)s.rows);
+    return 1400.0 + std::max(from_hbm, per_sm) + 60.0 * (double)((s.rows + c.warps - 1) / c.warps);
+}
+
+// One tile per cluster.
+double cost_few(const imat_plan_t *p, const CallShape &s, const MatChoice &c)
+{
+    const int kb = (p->k_blocks + c.split - 1) / c.split;
+    const bool two = c.smem <= (size_t)MAX_SMEM / 2 - 1024;
+    double at_once = (double)p->sms * (two ? 2 : 1);
+    if (c.split == 8 && !two) at_once = 0.75 * p->sms;         // (so many large blocks are seldom free within one part of the chip)
+    const double waves = std::max(1.0, std::ceil((double)c.grid / at_once));
+    const double per_sm = c.grid <= (unsigned)p->sms ? 1.0 : 0.5 * ((double)c.grid / p->sms + std::ceil((double)c.grid / p->sms));
+    const double load = std::max(per_sm * kb * c.stage_bytes / SM_RATE, waves * kb * ROUND_LATENCY / c.stages);
+    const double groups = std::ceil((double)std::min<long long>(c.nt, s.rows) / 16.0);
+    const double group = (p->gated ? 200.0 : 270.0) + 80.0 * s.act + 120.0 * s.residual;
+    const double epilogue = c.split == 1 ? groups * group : 700.0 + std::ceil(c.nt / 32.0) * 250.0 + std::ceil((double)c.nt / (16 * c.split)) * (group + 100.0);
+    return 1900.0 + (c.split > 1 ? 50.0 + 150.0 * c.split : 0.0) + std::max(std::max(load, waves * kb * ISSUE), s.hbm) + waves * epilogue + (waves - 1.0) * 1200.0;
+}
+
+// Persistent pairs: rounds of tiles, each bound by its sums or by the epilogue of the one before.
+double cost_bulk(const imat_plan_t *p, const CallShape &s, const MatChoice &c)
+{
+    const double tiles = (double)((p->ch_tiles + 1) / 2) * c.tok_tiles, rounds = std::ceil(tiles / (p->sms / 2));
+    const double sums = p->k_blocks * std::max((double)c.stage_bytes / SM_RATE, ISSUE);
+    const double epilogue = 1100.0 + c.nt / 64.0 * ((p->gated ? 560.0 : 600.0) + 500.0 * s.residual + 100.0 * s.act);
+    return std::max(2300.0 + sums + (rounds - 1.0) * std::max(sums, epilogue) + epilogue, 2300.0 + s.hbm);
+}
+
+MatChoice choose(const imat_plan_t *p, long long rows, bool residual)
+{
+    const CallShape s = shape_of(p, rows, residual);
+    MatChoice best = {};
+    double least = -1.0;
+    auto offer = [&](const MatChoice &c, double cost) {
+        if (c.smem <= (size_t)MAX_SMEM && (least < 0.0 || cost < least)) { least = cost; best = c; }
+    };
+    if (rows <= MAT_STREAM_TOKENS) {
+        const MatChoice c = choice_stream(p, rows);
+        offer(c, cost_stream(p, s, c));
     }
-    c.stage_bytes = MAT_BLOCK + c.nt / 2 * 128;
-    c.tmem_cols = 2 * MAT_BULK_TOKENS;
-    c.grid = 2u * (unsigned)std::min(ch_pairs * c.tok_tiles, pairs);
-    stages_of(c, MAT_ROOM, MAT_STAGES_MAX);
-    return c;
-}
-
-MatChoice choose(const imat_plan_t *p, long long rows)
-{
-    if ((long long)p->ch_tiles * ((rows + 127) / 128) <= 2 * p->sms) return choose_few(p, rows);
-    return choose_bulk(p, rows);
+    const long long tiles16 = (long long)p->ch_tiles * ((rows + 15) / 16);
+    for (int split = 1; split <= 8 && split <= p->k_blocks; split *= 2)
+        for (int nt : {16, 32, 48, 64, 96, 128}) {
+            if (nt >= rows + 16 && nt > 16) break;                 // the first that takes all rows is the last
+            if (tiles16 * 16 / nt * split > 8ll * p->sms) continue;
+            const MatChoice c = choice(p, rows, false, split, nt);
+            offer(c, cost_few(p, s, c));
+        }
+    for (int nt = 64; nt <= 256; nt += 32) {
+        const MatChoice c = choice(p, rows, true, 1, nt);
+        offer(c, cost_bulk(p, s, c));
+    }
+    return best;
 }
 
 int mat_opt_in(int *sms)
@@ -226,9 +297,10 @@ extern "C" int imat_plan(const imat_desc *desc, void *cuda_stream, imat_plan_t *
 extern "C" int imat_plan_describe(const imat_plan_t *p, int64_t rows, char *text, size_t size)
 {
     if (!p || !text || size == 0 || rows < 1 || rows > (1 << 30)) { set_error("imat_plan_describe: null argument or rows outside 1 ... 2^30"); return ICONV_ERR_ARG; }
-    const MatChoice c = choose(p, rows);
-    snprintf(text, size, "%s: tiles of %d channels x %d tokens, %u CTAs, split %d, %d stages of %d bytes%s", c.split ? "few" : "bulk", c.split ? 128 : 256, c.nt,
-             c.grid, c.split ? c.split : 1, c.stages, c.stage_bytes, p->gated ? ", gated" : "");
+    const MatChoice c = choose(p, rows, false);
+    if (c.streams) snprintf(text, size, "stream: tiles of %d rows x %d tokens, %u blocks of %d warps%s", MAT_STREAM_ROWS, c.nt, c.grid, c.warps, p->gated ? ", gated" : "");
+    else snprintf(text, size, "%s: tiles of %d channels x %d tokens, %u CTAs, split %d, %d stages of %d bytes%s", c.bulk ? "bulk" : "few", c.bulk ? 256 : 128,
+             c.nt, c.grid, c.split, c.stages, c.stage_bytes, p->gated ? ", gated" : "");
     return ICONV_OK;
 }
 
@@ -246,18 +318,21 @@ extern "C" int imat_forward(const imat_plan_t *p, int64_t rows, const int8_t *x,
     if ((uintptr_t)x % 16 || x_stride % 16 || (uintptr_t)x_scales % 16) { set_error("imat_forward: x and x_scales must be 16-byte aligned, x_stride a multiple of 16"); return ICONV_ERR_ALIGN; }
     if (((uintptr_t)out | (uintptr_t)residual) % element(p->out_dtype)) { set_error("imat_forward: out and residual must be aligned to their element"); return ICONV_ERR_ALIGN; }
     if (current_device_slot() != p->device) { set_error("imat_forward: the plan belongs to device %d, which is not current", p->device); return ICONV_ERR_ARG; }
-    const MatChoice c = choose(p, rows);
-    const int box = c.split ? c.nt : c.nt / 2;
+    const MatChoice c = choose(p, rows, residual != nullptr);
+    const int box = c.bulk ? c.nt / 2 : c.nt;
     CUtensorMap tmap_x;
-    const int rc = umma_encode_2d(&tmap_x, x, p->k, rows, x_stride, 128, box, 128);
-    if (rc != ICONV_OK) return rc;
+    if (!c.streams) {
+        const int rc = umma_encode_2d(&tmap_x, x, p->k, rows, x_stride, 128, box, 128);
+        if (rc != ICONV_OK) return rc;
+    }
+    const MatStreamArgs s = {p->packed, x, x_stride, (p->k - 1) / 16 * 16};
     MatArgs a;
     memset(&a, 0, sizeof(a));
     a.m = rows; a.n = p->n;
     a.ch_tiles = p->ch_tiles; a.tok_tiles = c.tok_tiles; a.nt = c.nt; a.k_blocks = p->k_blocks;
-    a.stages = c.stages; a.stage_bytes = c.stage_bytes; a.tmem_cols = c.tmem_cols;
+    a.stages = c.stages; a.stage_bytes = c.stage_bytes; a.split = c.split; a.recv_bytes = c.recv_bytes; a.tmem_cols = c.tmem_cols;
     // D = s32, A = s8, B = s8, both K-major, N / 8, M / 16 (a pair's instruction spans both CTAs' channels)
-    a.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(c.nt >> 3) << 17) | ((unsigned)((c.split ? BLOCK_M : 2 * BLOCK_M) >> 4) << 24);
+    a.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(c.nt >> 3) << 17) | ((unsigned)((c.bulk ? 2 * BLOCK_M : BLOCK_M) >> 4) << 24);
     a.act = p->act;
     a.row_params = p->row_params;
     a.x_scales = x_scales;
@@ -265,7 +340,8 @@ extern "C" int imat_forward(const imat_plan_t *p, int64_t rows, const int8_t *x,
     a.out = out; a.ld_out = out_stride;
     a.status = device_status_ptr();
     if (!a.status) { set_error("device status word not available"); return ICONV_ERR_CUDA; }
-    const MatLaunch l = {c.grid, c.smem, (cudaStream_t)cuda_stream, c.split, &p->tmap_w, &tmap_x, &a};
+    const unsigned threads = c.streams ? 32u * (unsigned)c.warps : c.bulk ? MAT_BULK_THREADS : MAT_FEW_THREADS;
+    const MatLaunch l = {c.grid, threads, c.smem, (cudaStream_t)cuda_stream, c.bulk, c.streams, &p->tmap_w, &tmap_x, &a, &s};
     const bool gated = p->gated != 0;
     ICONV_CUDA_TRY((p->out_dtype == ICONV_F32 ? mat_launch_0(gated, l) : p->out_dtype == ICONV_F16 ? mat_launch_1(gated, l) : mat_launch_2(gated, l)));
     return ICONV_OK;

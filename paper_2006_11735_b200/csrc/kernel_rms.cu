@@ -57,56 +57,51 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return d;
 }
 
-// VE consecutive elements at p: one 16-byte access where they are whole (VE * sizeof(T) = 16), else element by element
+// VE elements as they lie in memory: 16 bytes, or a single element
+template <typename T, int VE> struct Raw { uint4 w; };
+template <typename T> struct Raw<T, 1> { T w; };
+
 template <typename T, int VE>
-__device__ __forceinline__ void load_elems(const T *p, int count, float (&v)[VE])
+__device__ __forceinline__ Raw<T, VE> load_raw(const T *p)
 {
-    if (VE > 1 && count >= VE) {
-        const uint4 w = ld_tensor((const uint4 *)p);
-        const T *e = (const T *)&w;
-#pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = Elem<T>::to(e[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = j < count ? Elem<T>::to(p[j]) : 0.0f;
-    }
+    Raw<T, VE> v;
+    if constexpr (VE > 1) v.w = ld_tensor((const uint4 *)p);
+    else v.w = *p;
+    return v;
 }
 template <typename T, int VE>
-__device__ __forceinline__ void store_elems(T *p, int count, const float (&v)[VE])
+__device__ __forceinline__ void to_float(const Raw<T, VE> &v, float (&f)[VE])
 {
-    if (VE > 1 && count >= VE) {
-        uint4 w;
-        T *e = (T *)&w;
+    const T *e = (const T *)&v.w;
 #pragma unroll
-        for (int j = 0; j < VE; ++j) e[j] = Elem<T>::from(v[j]);
-        *(uint4 *)p = w;
-    } else {
+    for (int j = 0; j < VE; ++j) f[j] = Elem<T>::to(e[j]);
+}
+template <typename T, int VE>
+__device__ __forceinline__ void store_elems(T *p, const float (&f)[VE])
+{
+    Raw<T, VE> v;
+    T *e = (T *)&v.w;
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-            if (j < count) p[j] = Elem<T>::from(v[j]);
-    }
+    for (int j = 0; j < VE; ++j) e[j] = Elem<T>::from(f[j]);
+    if constexpr (VE > 1) *(uint4 *)p = v.w;
+    else *p = v.w;
 }
 // floor(v * inv + 1/2); the sum is rounded down, so that a value just under the border stays under it.  NaN gives 0.
 __device__ __forceinline__ int round_q(float v, float inv) { return __float2int_rd(__fadd_rd(__fmul_rn(v, inv), 0.5f)); }
 
 template <int VE>
-__device__ __forceinline__ void store_q(int8_t *p, int count, const float (&v)[VE], float inv)
+__device__ __forceinline__ void store_q(int8_t *p, const float (&v)[VE], float inv)
 {
-    int b[VE];
+    unsigned b[VE];
 #pragma unroll
-    for (int j = 0; j < VE; ++j) b[j] = round_q(v[j], inv);
-    if (VE >= 4 && count >= VE) {
+    for (int j = 0; j < VE; ++j) b[j] = (unsigned)round_q(v[j], inv);
+    if constexpr (VE > 1) {
 #pragma unroll
-        for (int w = 0; w < VE / 4; ++w) {
-            const unsigned lo = __byte_perm((unsigned)b[4 * w], (unsigned)b[4 * w + 1], 0x0040), hi = __byte_perm((unsigned)b[4 * w + 2], (unsigned)b[4 * w + 3], 0x0040);
-            b[w] = (int)__byte_perm(lo, hi, 0x5410);
-        }
-        if (VE == 8) *(uint2 *)p = make_uint2((unsigned)b[0], (unsigned)b[1]);
-        else *(unsigned *)p = (unsigned)b[0];
+        for (int w = 0; w < VE / 4; ++w) b[w] = __byte_perm(__byte_perm(b[4 * w], b[4 * w + 1], 0x0040), __byte_perm(b[4 * w + 2], b[4 * w + 3], 0x0040), 0x5410);
+        if constexpr (VE == 8) *(uint2 *)p = make_uint2(b[0], b[1]);
+        else *(unsigned *)p = b[0];
     } else {
-#pragma unroll
-        for (int j = 0; j < VE; ++j)
-            if (j < count) p[j] = (int8_t)b[j];
+        *p = (int8_t)b[0];
     }
 }
 
@@ -154,27 +149,26 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
     const T *r = a.r ? (const T *)a.r + row * a.ldr : nullptr;
     T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
     int8_t *q = a.q + row * a.ldq;
+    const int vecs = a.width / VE;
     RowSums m = {0.0f, 0.0f, 0.0f};
 
-    // s of the VE elements from `at` on; nothing beyond the row's end
-    auto fetch = [&](int at, float (&s)[VE]) {
-        const int count = a.width - at;
-        load_elems<T, VE>(x + at, count, s);
+    // s of a vector, from what was loaded of x and the residual
+    auto add = [&](const Raw<T, VE> &xr, const Raw<T, VE> &rr, float (&s)[VE]) {
+        to_float<T, VE>(xr, s);
         if (r) {
             float o[VE];
-            load_elems<T, VE>(r + at, count, o);
+            to_float<T, VE>(rr, o);
 #pragma unroll
             for (int j = 0; j < VE; ++j) s[j] = __fadd_rn(s[j], o[j]);
         }
     };
-    auto weigh = [&](int at, float (&s)[VE]) {
-        const int count = a.width - at;
+    auto weigh = [&](int i, const Raw<T, VE> &gr, float (&s)[VE]) {
         if (a.g && a.g_f32) {
 #pragma unroll
-            for (int j = 0; j < VE; ++j) s[j] = j < count ? __fmul_rn(s[j], ((const float *)a.g)[at + j]) : 0.0f;
+            for (int j = 0; j < VE; ++j) s[j] = __fmul_rn(s[j], ((const float *)a.g)[i * VE + j]);
         } else if (a.g) {
             float g[VE];
-            load_elems<T, VE>((const T *)a.g + at, count, g);
+            to_float<T, VE>(gr, g);
 #pragma unroll
             for (int j = 0; j < VE; ++j) s[j] = __fmul_rn(s[j], g[j]);
         }
@@ -183,36 +177,45 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
             m.sq = fmaf(s[j], s[j], m.sq);
-            if (sizeof(T) == 4 || !std::is_same<T, __half>::value) m.sq_down = fmaf(s[j] * DOWN, s[j] * DOWN, m.sq_down);      // (no sum of two halves needs it)
+            if (!std::is_same<T, __half>::value) m.sq_down = fmaf(s[j] * DOWN, s[j] * DOWN, m.sq_down);      // (no sum of two halves needs it)
         }
     };
     auto largest = [&](const float (&v)[VE]) {
 #pragma unroll
         for (int j = 0; j < VE; ++j) m.top = max_nan(m.top, fabsf(v[j]));
     };
+    // vector i of x, the residual and the weight; each load is issued whether or not the thread has such a vector (it then reads the
+    // last one), so that none waits behind a branch for the one before it
+    auto fetch = [&](int i, Raw<T, VE> &xr, Raw<T, VE> &rr, Raw<T, VE> &gr) {
+        const int at = (i < vecs ? i : vecs - 1) * VE;
+        xr = load_raw<T, VE>(x + at);
+        if (r) rr = load_raw<T, VE>(r + at);
+        if (a.g && !a.g_f32) gr = load_raw<T, VE>((const T *)a.g + at);
+    };
 
     float v[HELD][VE];
     if (R > 0) {
+        Raw<T, VE> xr[HELD], rr[HELD], gr[HELD];
+#pragma unroll
+        for (int i = 0; i < R; ++i) fetch(i * TPR + t, xr[i], rr[i], gr[i]);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int at = (i * TPR + t) * VE;
-            if (at < a.width) fetch(at, v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int at = (i * TPR + t) * VE;
-            if (at < a.width) {
-                if (out) store_elems<T, VE>(out + at, a.width - at, v[i]);
+            const int at = i * TPR + t;
+            if (at < vecs) {
+                add(xr[i], rr[i], v[i]);
+                if (out) store_elems<T, VE>(out + at * VE, v[i]);
                 squares(v[i]);
-                weigh(at, v[i]);
+                weigh(at, gr[i], v[i]);
                 largest(v[i]);
             }
         }
     } else {
-        for (int at = t * VE; at < a.width; at += TPR * VE) {
-            fetch(at, v[0]);
+        for (int at = t; at < vecs; at += TPR) {
+            Raw<T, VE> xr, rr, gr;
+            fetch(at, xr, rr, gr);
+            add(xr, rr, v[0]);
             squares(v[0]);
-            weigh(at, v[0]);
+            weigh(at, gr, v[0]);
             largest(v[0]);
         }
     }
@@ -232,15 +235,17 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
     if (R > 0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int at = (i * TPR + t) * VE;
-            if (at < a.width) store_q<VE>(q + at, a.width - at, v[i], inv);
+            const int at = i * TPR + t;
+            if (at < vecs) store_q<VE>(q + at * VE, v[i], inv);
         }
     } else {
-        for (int at = t * VE; at < a.width; at += TPR * VE) {
-            fetch(at, v[0]);
-            if (out) store_elems<T, VE>(out + at, a.width - at, v[0]);       // (only now: it may be where x or the residual is)
-            weigh(at, v[0]);
-            store_q<VE>(q + at, a.width - at, v[0], inv);
+        for (int at = t; at < vecs; at += TPR) {
+            Raw<T, VE> xr, rr, gr;
+            fetch(at, xr, rr, gr);
+            add(xr, rr, v[0]);
+            if (out) store_elems<T, VE>(out + at * VE, v[0]);       // (only now: it may be where x or the residual is)
+            weigh(at, gr, v[0]);
+            store_q<VE>(q + at * VE, v[0], inv);
         }
     }
 }
@@ -257,7 +262,7 @@ cudaError_t launch_one(const RmsArgs &a, cudaStream_t stream)
 template <typename T, int VE>
 cudaError_t launch_width(const RmsArgs &a, cudaStream_t stream)
 {
-    const int vecs = (a.width + VE - 1) / VE;
+    const int vecs = a.width / VE;
     if constexpr (VE > 1) {
         if (vecs <= 32) return launch_one<T, VE, 32, 1>(a, stream);
         if (vecs <= 64) return launch_one<T, VE, 32, 2>(a, stream);
@@ -326,7 +331,7 @@ extern "C" int irms_quant(const irms_desc *desc, const void *x, const void *resi
     a.rows = d.rows; a.ldx = d.x_stride; a.ldr = d.residual_stride; a.lds = d.sum_stride; a.ldq = d.q_stride;
     a.width = d.width; a.g_f32 = d.weight_dtype == ICONV_F32; a.norm = d.norm; a.eps = d.eps; a.inv_width = 1.0f / (float)d.width;
     const int ve = 16 / e;                                          // elements of a vector; the same number of bytes of q
-    bool whole = !(((uintptr_t)x | (uintptr_t)residual | (uintptr_t)sum) % 16) && !((uintptr_t)q % ve) && !(d.x_stride % ve) && !(d.q_stride % ve);
+    bool whole = !(d.width % ve) && !(((uintptr_t)x | (uintptr_t)residual | (uintptr_t)sum) % 16) && !((uintptr_t)q % ve) && !(d.x_stride % ve) && !(d.q_stride % ve);
     if (residual) whole = whole && !(d.residual_stride % ve);
     if (sum) whole = whole && !(d.sum_stride % ve);
     if (weight && !(a.g_f32 && d.dtype != ICONV_F32)) whole = whole && !((uintptr_t)weight % 16);

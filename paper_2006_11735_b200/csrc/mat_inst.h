@@ -2,16 +2,18 @@
 #pragma once
 
 #include "mat_device.cuh"
+#include "mat_stream.cuh"
 
 namespace iconv {
 
 struct MatLaunch {
-    unsigned grid;
+    unsigned grid, threads;
     size_t smem;
     cudaStream_t stream;
-    int split;                      // 0: the bulk kernel; else the few-token kernel's CTAs per tile (1, 2, 4 or 8)
+    bool bulk, streams;             // the bulk kernel, the streaming kernel, else the few-tile kernel
     const CUtensorMap *tmap_w, *tmap_x;
     const MatArgs *a;
+    const MatStreamArgs *s;
 };
 
 #define ICONV_DECLARE_MAT(E) cudaError_t mat_launch_##E(bool gated, const MatLaunch &l); cudaError_t mat_opt_in_##E();

@@ -31,11 +31,13 @@ def test_sizes(gated, k, n):
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("m", [2, 2100])
-def test_epilogues(dtype, act, gated, m):
-    """Few rows and many: either kernel with every activation, type and form."""
-    plan, x, sx, r = _case(1, m, 640, 2336, dtype, act, gated, residual=not gated)
-    assert plan.describe(m).startswith("few" if m == 2 else "bulk")
+@pytest.mark.parametrize("m,k,kernel", [(2, 640, "stream"), (11, 640, "stream"), (40, 640, "few"), (100, 4096, "few"), (2100, 640, "bulk")])
+def test_epilogues(dtype, act, gated, m, k, kernel):
+    """Every kernel (of the few-tile one the forms that share a reduction and that do not) with every activation, type and form."""
+    plan, x, sx, r = _case(1, m, k, 2336, dtype, act, gated, residual=not gated)
+    assert plan.describe(m).startswith(kernel)
+    if kernel == "few" and not gated:
+        assert ("split 1," in plan.describe(m)) == (m == 40)
     plan.check(x, sx, plan(x, sx, r), r)
     if not gated:
         plan.check(x, sx, plan(x, sx))
@@ -109,8 +111,8 @@ def test_a_row_is_the_same_in_any_call(gated, dtype):
     plan, x, sx, r = _case(7, 2500, 1030, 2500, dtype, "silu", gated, residual=not gated)
     whole = plan(x, sx, r)
     assert plan.describe(2500).startswith("bulk")
-    for m in (1, 9, 64, 200):
-        assert plan.describe(m).startswith("few")
+    for m, kernel in ((1, "stream"), (9, "stream"), (64, "few"), (100, "few")):
+        assert plan.describe(m).startswith(kernel)
         for at in (0, 1200):
             some = plan(x[at:at + m], sx[at:at + m].clone(), r[at:at + m] if r is not None else None)
             assert torch.equal(some, whole[at:at + m]), (m, at)
