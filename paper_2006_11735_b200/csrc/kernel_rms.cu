@@ -8,14 +8,15 @@
 //
 // What bounds it: HBM -- 7 bytes an element with a residual in 16 bits.  One block per row (a warp per row for short ones), vectors of
 // 16 bytes per thread.
+#include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <cstdint>
-#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "plan.h"
+#include "umma_device.cuh"
 
 namespace iconv {
 
@@ -43,10 +44,14 @@ template <> struct Elem<float> {
 template <> struct Elem<__half> {
     static __device__ __forceinline__ float to(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half from(float v) { return __float2half_rn(v); }
+    using Two = __half2;
+    static __device__ __forceinline__ Two from2(float a, float b) { return __floats2half2_rn(a, b); }
 };
 template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ float to(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
+    using Two = __nv_bfloat162;
+    static __device__ __forceinline__ Two from2(float a, float b) { return __floats2bfloat162_rn(a, b); }
 };
 
 // the larger of the two, NaN if either is
@@ -79,35 +84,67 @@ __device__ __forceinline__ void to_float(const Raw<T, VE> &v, float (&f)[VE])
 template <typename T, int VE>
 __device__ __forceinline__ void store_elems(T *p, const float (&f)[VE])
 {
-    Raw<T, VE> v;
-    T *e = (T *)&v.w;
+    if constexpr (VE == 8) {
+        using Two = typename Elem<T>::Two;
+        union { Two t[4]; uint4 w; } v;
 #pragma unroll
-    for (int j = 0; j < VE; ++j) e[j] = Elem<T>::from(f[j]);
-    if constexpr (VE > 1) *(uint4 *)p = v.w;
-    else *p = v.w;
+        for (int j = 0; j < 4; ++j) v.t[j] = Elem<T>::from2(f[2 * j], f[2 * j + 1]);
+        *(uint4 *)p = v.w;
+    } else if constexpr (VE == 4) {
+        *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+        *p = Elem<T>::from(f[0]);
+    }
 }
-// floor(v * inv + 1/2); the sum is rounded down, so that a value just under the border stays under it.  NaN gives 0.
-__device__ __forceinline__ int round_q(float v, float inv) { return __float2int_rd(__fadd_rd(__fmul_rn(v, inv), 0.5f)); }
+// floor(v * inv + 1/2) in the low byte: both sums are rounded down, the first so that a value just under the border stays under it, the second
+// leaves the whole number beside 1.5 * 2^23 (an addition where a conversion runs at an eighth of the rate).  For |v * inv| of 127 and a rounding.
+__device__ __forceinline__ unsigned round_q(float v, float inv) { return __float_as_uint(__fadd_rd(__fadd_rd(__fmul_rn(v, inv), 0.5f), 12582912.0f)); }
 
+// inv = 0 (nothing in the row, or something that is no number): zeros
 template <int VE>
 __device__ __forceinline__ void store_q(int8_t *p, const float (&v)[VE], float inv)
 {
     unsigned b[VE];
 #pragma unroll
-    for (int j = 0; j < VE; ++j) b[j] = (unsigned)round_q(v[j], inv);
+    for (int j = 0; j < VE; ++j) b[j] = round_q(v[j], inv);
     if constexpr (VE > 1) {
 #pragma unroll
-        for (int w = 0; w < VE / 4; ++w) b[w] = __byte_perm(__byte_perm(b[4 * w], b[4 * w + 1], 0x0040), __byte_perm(b[4 * w + 2], b[4 * w + 3], 0x0040), 0x5410);
+        for (int w = 0; w < VE / 4; ++w) {
+            b[w] = __byte_perm(__byte_perm(b[4 * w], b[4 * w + 1], 0x0040), __byte_perm(b[4 * w + 2], b[4 * w + 3], 0x0040), 0x5410);
+            if (inv == 0.0f) b[w] = 0;
+        }
         if constexpr (VE == 8) *(uint2 *)p = make_uint2(b[0], b[1]);
         else *(unsigned *)p = b[0];
     } else {
-        *p = (int8_t)b[0];
+        *p = inv == 0.0f ? (int8_t)0 : (int8_t)b[0];
     }
 }
 
-// What a row's threads gather: the sum of squares, the same of the values 2^-100 of themselves (finite where the other is not), the largest magnitude.
+// What a row's threads gather: the sum of squares; the same of the values 2^-100 of themselves, for the case that the other does not fit, over the
+// threads whose squares pass 1e25 (what the others hold is nothing beside a sum that does not fit); the largest magnitude.
 struct RowSums {
     float sq, sq_down, top;
+    template <int R, int VE>
+    __device__ __forceinline__ void squares(const float (&s)[R][VE])        // (of a thread's whole share: one look at the sum)
+    {
+        float p = 0.0f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < VE; ++j) p = fmaf(s[i][j], s[i][j], p);
+        sq += p;
+        if (p > 1.0e25f)
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < VE; ++j) sq_down = fmaf(s[i][j] * DOWN, s[i][j] * DOWN, sq_down);
+    }
+    template <int VE>
+    __device__ __forceinline__ void largest(const float (&v)[VE])
+    {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) top = max_nan(top, fabsf(v[j]));
+    }
     __device__ __forceinline__ void join(const RowSums &o)
     {
         sq += o.sq;
@@ -130,6 +167,21 @@ __device__ __forceinline__ void row_reduce(RowSums &m, RowSums *sh)
 #pragma unroll
         for (int w = 1; w < TPR / 32; ++w) m.join(sh[w]);
     }
+}
+
+// The row's scale (stored by `stores`), and what v is multiplied by before it is rounded.
+__device__ __forceinline__ float finish_row(const RmsArgs &a, const RowSums &m, long long row, bool stores)
+{
+    const bool broken = !(m.top <= FLT_MAX);                       // a NaN or an infinity in the row
+    const bool empty = m.top < TINY_ROW;
+    float scale = m.top * (1.0f / 127.0f);
+    if (a.norm) {
+        // (where the squares of finite values do not fit, eps is nothing beside them)
+        if (m.sq <= FLT_MAX) scale *= 1.0f / sqrtf(fmaf(m.sq, a.inv_width, a.eps));
+        else scale = scale * DOWN / sqrtf(m.sq_down * a.inv_width);
+    }
+    if (stores) a.scales[row] = broken ? __int_as_float(0x7fffffff) : empty ? 0.0f : scale;
+    return broken || empty ? 0.0f : __fdiv_rn(127.0f, m.top);
 }
 
 // TPR threads a row, R vectors of VE elements each in registers (R = 0: any width, the row is read twice).
@@ -173,17 +225,6 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             for (int j = 0; j < VE; ++j) s[j] = __fmul_rn(s[j], g[j]);
         }
     };
-    auto squares = [&](const float (&s)[VE]) {
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            m.sq = fmaf(s[j], s[j], m.sq);
-            if (!std::is_same<T, __half>::value) m.sq_down = fmaf(s[j] * DOWN, s[j] * DOWN, m.sq_down);      // (no sum of two halves needs it)
-        }
-    };
-    auto largest = [&](const float (&v)[VE]) {
-#pragma unroll
-        for (int j = 0; j < VE; ++j) m.top = max_nan(m.top, fabsf(v[j]));
-    };
     // vector i of x, the residual and the weight; each load is issued whether or not the thread has such a vector (it then reads the
     // last one), so that none waits behind a branch for the one before it
     auto fetch = [&](int i, Raw<T, VE> &xr, Raw<T, VE> &rr, Raw<T, VE> &gr) {
@@ -204,9 +245,26 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             if (at < vecs) {
                 add(xr[i], rr[i], v[i]);
                 if (out) store_elems<T, VE>(out + at * VE, v[i]);
-                squares(v[i]);
-                weigh(at, gr[i], v[i]);
-                largest(v[i]);
+                if constexpr (VE == 1) {            // (both sums as they come cost a thread of single elements less than a second loop)
+                    m.sq = fmaf(v[i][0], v[i][0], m.sq);
+                    m.sq_down = fmaf(v[i][0] * DOWN, v[i][0] * DOWN, m.sq_down);
+                    weigh(at, gr[i], v[i]);
+                    m.largest(v[i]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < VE; ++j) v[i][j] = 0.0f;
+            }
+        }
+        if constexpr (VE > 1) {
+            m.squares(v);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int at = i * TPR + t;
+                if (at < vecs) {
+                    weigh(at, gr[i], v[i]);
+                    m.largest(v[i]);
+                }
             }
         }
     } else {
@@ -214,23 +272,14 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             Raw<T, VE> xr, rr, gr;
             fetch(at, xr, rr, gr);
             add(xr, rr, v[0]);
-            squares(v[0]);
+            m.squares(v);
             weigh(at, gr, v[0]);
-            largest(v[0]);
+            m.largest(v[0]);
         }
     }
     row_reduce<TPR>(m, sh);
 
-    const bool broken = !(m.top <= FLT_MAX);                       // a NaN or an infinity in the row
-    const bool empty = m.top < TINY_ROW;
-    float scale = m.top * (1.0f / 127.0f);
-    if (a.norm) {
-        // (where the squares of finite values do not fit, eps is nothing beside them)
-        if (m.sq <= FLT_MAX) scale *= 1.0f / sqrtf(fmaf(m.sq, a.inv_width, a.eps));
-        else scale = scale * DOWN / sqrtf(m.sq_down * a.inv_width);
-    }
-    const float inv = broken || empty ? 0.0f : __fdiv_rn(127.0f, m.top);
-    if (t == 0) a.scales[row] = broken ? __int_as_float(0x7fffffff) : empty ? 0.0f : scale;
+    const float inv = finish_row(a, m, row, t == 0);
 
     if (R > 0) {
 #pragma unroll
@@ -247,6 +296,147 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             weigh(at, gr, v[0]);
             store_q<VE>(q + at * VE, v[0], inv);
         }
+    }
+}
+
+// Many wide rows: one block per SM, whose loading warps keep a ring of whole rows in shared memory ahead of the arithmetic, so that the memory
+// stays busy while a row is being reduced (a block per row has nothing in flight then: 4096 rows of 16384 in bfloat16 took 86 us, 46 this
+// way, floor 31).  Groups of GW warps take the rows in turn, ELEMS elements a thread; a group meets at one named barrier per row.  The ring's stages
+// are a multiple of the groups, so that a stage always holds rows of one group, which has taken the one before when it waits for the next (the
+// loads may complete in any order, and a parity cannot tell two rows apart).
+constexpr int STREAM_WARPS = 16;                    // that do the arithmetic
+constexpr int STREAM_LOADERS = 2;                   // warp 0 loads x, warp 1 the residual
+constexpr int STREAM_STAGES_MAX = 16;
+
+struct StreamShared {
+    unsigned long long full[STREAM_STAGES_MAX], empty[STREAM_STAGES_MAX];
+    RowSums sums[2][STREAM_WARPS];
+    volatile int abort_flag;
+};
+
+struct StreamArgs {
+    RmsArgs a;
+    int stages, row_bytes, stage_bytes;             // row_bytes: of x, and of the residual
+    int *status;
+};
+
+template <typename T, int GW, int ELEMS>
+__global__ void __launch_bounds__(32 * (STREAM_WARPS + STREAM_LOADERS), 1) rms_stream_kernel(const __grid_constant__ StreamArgs s)
+{
+    constexpr int VE = 16 / (int)sizeof(T), R = ELEMS / VE, GROUPS = STREAM_WARPS / GW, TPR = 32 * GW;
+    extern __shared__ __align__(16) uint8_t ring[];
+    StreamShared *sh = (StreamShared *)(ring + (size_t)s.stages * s.stage_bytes);
+    const RmsArgs &a = s.a;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    if (warp == 0) {
+        if (lane < s.stages) {
+            mbar_init(smem_u32(&sh->full[lane]), a.r ? 2 : 1);
+            mbar_init(smem_u32(&sh->empty[lane]), GW);
+        }
+        if (lane == 0) sh->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    grid_dep_launch();
+    grid_dep_wait();
+    const long long rows = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;        // of this block: blockIdx.x, + gridDim.x, ...
+    auto gave_up = [&](int code) {
+        sh->abort_flag = 1;
+        atomicCAS(s.status, 0, code);
+    };
+    if (warp < STREAM_LOADERS) {
+        if (lane == 0 && (warp == 0 || a.r)) {
+            const char *src = (const char *)(warp == 0 ? a.x : a.r) + (long long)blockIdx.x * (warp == 0 ? a.ldx : a.ldr) * (long long)sizeof(T);
+            const long long step = (long long)gridDim.x * (warp == 0 ? a.ldx : a.ldr) * (long long)sizeof(T);
+            int stage = 0;
+            uint32_t parity = 0;
+            for (long long j = 0; j < rows; ++j, src += step) {
+                if (!mbar_wait(smem_u32(&sh->empty[stage]), parity ^ 1u, &sh->abort_flag)) { gave_up(1); break; }
+                const uint32_t full = smem_u32(&sh->full[stage]);
+                mbar_expect_tx(full, (uint32_t)s.row_bytes);
+                bulk_load(smem_u32(ring + (size_t)stage * s.stage_bytes + (warp ? s.row_bytes : 0)), src, (uint32_t)s.row_bytes, full);
+                if (++stage == s.stages) { stage = 0; parity ^= 1u; }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int group = (warp - STREAM_LOADERS) / GW, in_group = (warp - STREAM_LOADERS) % GW, t = in_group * 32 + lane;
+        const int vecs = a.width / VE;
+        constexpr bool HELD = ELEMS <= 32;          // the weights of this thread's elements, the same for every row, stay in registers
+        uint4 g[HELD ? R : 1];
+        if (HELD && a.g && !a.g_f32)
+#pragma unroll
+            for (int i = 0; i < R; ++i) g[HELD ? i : 0] = ld_tensor((const uint4 *)((const T *)a.g + (i * TPR + t < vecs ? i * TPR + t : vecs - 1) * VE));
+        int stage = group % s.stages, turn = 0;
+        uint32_t parity = (uint32_t)(group / s.stages) & 1u;
+        // (a wait that runs out leaves its mark and the loop goes on with what there is: every thread meets its group's barrier as often as the others)
+        for (long long j = group; j < rows; j += GROUPS, turn ^= 1) {
+            const long long row = blockIdx.x + j * gridDim.x;
+            if (!mbar_wait(smem_u32(&sh->full[stage]), parity, &sh->abort_flag)) gave_up(2);
+            const uint32_t at = smem_u32(ring + (size_t)stage * s.stage_bytes) + (uint32_t)(t * 16);
+            T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
+            RowSums m = {0.0f, 0.0f, 0.0f};
+            float v[R][VE];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (i * TPR + t < vecs) {
+                    Raw<T, VE> raw;
+                    raw.w = lds128(at + (uint32_t)(i * TPR * 16));
+                    to_float<T, VE>(raw, v[i]);
+                    if (a.r) {
+                        float o[VE];
+                        raw.w = lds128(at + (uint32_t)(s.row_bytes + i * TPR * 16));
+                        to_float<T, VE>(raw, o);
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) v[i][e] = __fadd_rn(v[i][e], o[e]);
+                    }
+                    if (out) store_elems<T, VE>(out + (i * TPR + t) * VE, v[i]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) v[i][e] = 0.0f;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->empty[stage]));             // the row is in registers
+            m.squares(v);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (i * TPR + t < vecs) {
+                    if (a.g && a.g_f32) {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) v[i][e] = __fmul_rn(v[i][e], ((const float *)a.g)[(i * TPR + t) * VE + e]);
+                    } else if (a.g) {
+                        Raw<T, VE> raw;
+                        float w[VE];
+                        raw.w = HELD ? g[HELD ? i : 0] : ld_tensor((const uint4 *)((const T *)a.g + (i * TPR + t) * VE));
+                        to_float<T, VE>(raw, w);
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) v[i][e] = __fmul_rn(v[i][e], w[e]);
+                    }
+                    m.largest(v[i]);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                m.join({__shfl_xor_sync(0xffffffffu, m.sq, o), __shfl_xor_sync(0xffffffffu, m.sq_down, o), __shfl_xor_sync(0xffffffffu, m.top, o)});
+            if (lane == 0) sh->sums[turn][warp - STREAM_LOADERS] = m;
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(TPR) : "memory");
+            m = sh->sums[turn][group * GW];
+#pragma unroll
+            for (int w = 1; w < GW; ++w) m.join(sh->sums[turn][group * GW + w]);
+            const float inv = finish_row(a, m, row, t == 0);
+            int8_t *q = a.q + row * a.ldq;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (i * TPR + t < vecs) store_q<VE>(q + (i * TPR + t) * VE, v[i], inv);
+            for (int skip = 0; skip < GROUPS; ++skip)
+                if (++stage == s.stages) { stage = 0; parity ^= 1u; }
+        }
+    }
+    __syncthreads();
+    if (sh->abort_flag && threadIdx.x == 0) {       // whatever is still on its way into this block's memory
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000) {}
     }
 }
 
@@ -282,10 +472,76 @@ cudaError_t launch_width(const RmsArgs &a, cudaStream_t stream)
     }
 }
 
+using StreamKernel = void (*)(StreamArgs);
+
+// Groups that a block's warps make for rows of a width: eight of two warps, four or two, 32 elements a thread; the widest rows take 64 a thread, so that
+// two groups can still take turns (4096 rows of 16384 without a residual: 46 us, 58 in one group).
+constexpr int STREAM_WIDTH_MAX = 8 * 32 * 64;
+int stream_groups(int width) { return width <= 2 * 32 * 32 ? 8 : width <= 4 * 32 * 32 ? 4 : 2; }
+template <typename T>
+StreamKernel stream_kernel(int width)
+{
+    switch (stream_groups(width)) {
+    case 8: return rms_stream_kernel<T, 2, 32>;
+    case 4: return rms_stream_kernel<T, 4, 32>;
+    default: return width <= 8 * 32 * 32 ? rms_stream_kernel<T, 8, 32> : rms_stream_kernel<T, 8, 64>;
+    }
+}
+
+// Shared-memory opt-in of the current device, once; its SM count.
+int stream_opt_in(int *sms)
+{
+    static std::atomic<int> count[MAX_DEVICES];
+    const int dev = current_device_slot();
+    if (dev < 0) { set_error("irms_quant: no current device, or its index is beyond %d", MAX_DEVICES - 1); return ICONV_ERR_UNSUPPORTED; }
+    if (!count[dev].load(std::memory_order_acquire)) {
+        for (int width = 2048; width <= STREAM_WIDTH_MAX; width *= 2)
+            for (StreamKernel k : {stream_kernel<float>(width), stream_kernel<__half>(width), stream_kernel<__nv_bfloat16>(width)})
+                ICONV_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
+        int n = 0;
+        ICONV_CUDA_TRY(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
+        count[dev].store(n, std::memory_order_release);
+    }
+    *sms = count[dev].load(std::memory_order_acquire);
+    return ICONV_OK;
+}
+
+// Rows of 8 KB or more, with a residual 16 KB (there a block per row has enough in flight: 8192 rows of 4096 in bfloat16 take 38 us so, 44 as a
+// stream; without the residual 27 and 27, 4096 rows of 8192 36 and 28), of which the ring takes one for every group and three at least; four
+// rows or more for every SM.
+bool streams(const RmsArgs &a, int element)
+{
+    const long long bytes = (long long)a.width * element, most = MAX_SMEM - (long long)sizeof(StreamShared);
+    const bool residual = a.r != nullptr;
+    return bytes >= (residual ? 16384 : 8192) && a.width <= STREAM_WIDTH_MAX && a.rows >= 4 * 148 &&
+           std::max(3, stream_groups(a.width)) * bytes * (residual ? 2 : 1) <= most;
+}
+
+template <typename T>
+int launch_stream(const RmsArgs &a, cudaStream_t stream)
+{
+    int sms = 0;
+    const int rc = stream_opt_in(&sms);
+    if (rc != ICONV_OK) return rc;
+    StreamArgs s;
+    s.a = a;
+    s.row_bytes = a.width * (int)sizeof(T);
+    s.stage_bytes = s.row_bytes * (a.r ? 2 : 1);
+    const int groups = stream_groups(a.width);
+    s.stages = std::min((MAX_SMEM - (int)sizeof(StreamShared)) / s.stage_bytes, STREAM_STAGES_MAX) / groups * groups;
+    s.status = device_status_ptr();
+    if (!s.status) { set_error("device status word not available"); return ICONV_ERR_CUDA; }
+    const auto kernel = stream_kernel<T>(a.width);
+    ICONV_CUDA_TRY(launch_kernel(kernel, true, (unsigned)std::min<long long>(a.rows, sms), 32 * (STREAM_WARPS + STREAM_LOADERS),
+                                 (size_t)s.stages * s.stage_bytes + sizeof(StreamShared), stream, s));
+    return ICONV_OK;
+}
+
 template <typename T>
 int launch_rms(const RmsArgs &a, bool whole, cudaStream_t stream)
 {
     constexpr int VE = 16 / (int)sizeof(T);
+    if (whole && streams(a, (int)sizeof(T))) return launch_stream<T>(a, stream);
     ICONV_CUDA_TRY((whole ? launch_width<T, VE>(a, stream) : launch_width<T, 1>(a, stream)));
     return ICONV_OK;
 }

@@ -153,3 +153,37 @@ def test_no_rows():
     x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
     B.irms_quant(None, None, None, None, None, None, stream(), rows=0, width=64, dtype=B.BF16)
     assert rms_call(x)[0].shape == (0, 64) and ptr(x) is not None
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 4096), ("bf16", 4608), ("bf16", 9000), ("f16", 8192), ("bf16", 16384), ("f32", 2048), ("f32", 4100), ("f32", 8192), ("f16", 12008), ("f32", 16384),
+                                     ("f32", 16380)])
+@pytest.mark.parametrize("residual,weight,norm", [(True, "same", 1), (False, "f32", 1), (False, None, 0), (True, None, 1)])
+def test_many_wide_rows(dtype, d, residual, weight, norm):
+    """Rows that stream through shared memory, several for every block and not the same number for all; the same rows a block each."""
+    m = 148 * 5 + 37
+    x, r, g = _data(d, m, d, dtype, residual, weight)
+    x[700, d - 1] = float("nan")
+    q, scales, total = rms_call(x, r, g, norm=norm)
+    keep = torch.arange(m, device="cuda") != 700
+    assert torch.isnan(scales[700]) and (q[700] == 0).all()
+    rms_check(x[keep], r[keep] if residual else None, g, q[keep], scales[keep], total[keep], norm=norm)
+    for at in (0, 300, m - 20):
+        a, b, c = rms_call(x[at:at + 20], r[at:at + 20] if residual else None, g, norm=norm)
+        same = keep[at:at + 20]
+        assert torch.equal(a, q[at:at + 20]) and torch.equal(c[same], total[at:at + 20][same])
+        assert ((b - scales[at:at + 20]).abs()[same] <= 40 * 2.0 ** -24 * b[same]).all()       # (the squares are added in another order)
+    B.iconv_check(stream())
+
+
+def test_many_wide_rows_in_place_and_with_strides():
+    m, d = 148 * 6 + 1, 5000
+    x, r, g = _data(3, m, d, "bf16", pad=24)
+    r = (2 * torch.randn(m, d + 8, generator=generator(4), device="cuda")).bfloat16()[:, :d]
+    want = rms_call(x, r, g)
+    rms_check(x, r, g, *want)
+    for into in (x.clone(memory_format=torch.preserve_format), r.clone(memory_format=torch.preserve_format)):
+        q_store = torch.full((m, d + 40), 77, dtype=torch.int8, device="cuda")
+        first = into.shape == x.shape and torch.equal(into, x)
+        q, scales, total = rms_call(into if first else x, r if first else into, g, q=q_store[:, :d], total=into)
+        assert torch.equal(q, want[0]) and torch.equal(scales, want[1]) and torch.equal(total, want[2]) and (q_store[:, d:] == 77).all()
+    B.iconv_check(stream())
