@@ -371,7 +371,8 @@ ICONV_API int irms_quant(const irms_desc *desc, const void *x, const void *resid
  * int32 whatever the values).
  * imat_forward: a plan belongs to its device, which must be current.  It enqueues one kernel, needs no workspace and keeps nothing: calls of
  * one plan may overlap on any streams and may be captured.
- *   x          DEVICE int8 rows x k, 16-byte aligned, x_stride a multiple of 16 (k itself may be anything)
+ *   x          DEVICE int8 rows x k, 16-byte aligned, x_stride a multiple of 16 (k itself may be anything; the bytes from k to the next
+ *              multiple of 16 may be read, in the last row too, and are not used)
  *   x_scales   DEVICE float [rows], 16-byte aligned
  *   residual   DEVICE rows x n of out_dtype, or NULL; may be out itself at the same stride.  Not with a gated plan (ICONV_ERR_UNSUPPORTED)
  *   out        DEVICE rows x n of out_dtype; out and residual are aligned to their element
@@ -402,7 +403,7 @@ ICONV_API int imat_plan(const imat_desc *desc, void *cuda_stream, imat_plan_t **
 ICONV_API int imat_plan_destroy(imat_plan_t *plan);
 ICONV_API int imat_forward(const imat_plan_t *plan, int64_t rows, const int8_t *x, int64_t x_stride, const float *x_scales,
                            const void *residual, int64_t residual_stride, void *out, int64_t out_stride, void *cuda_stream);
-/* One line of text on how a call of `rows` rows runs (kernel, tile, split), as iconv_plan_describe. */
+/* One line of text on how a call of `rows` rows without a residual runs (kernel, tile, split), as iconv_plan_describe. */
 ICONV_API int imat_plan_describe(const imat_plan_t *plan, int64_t rows, char *text, size_t size);
 
 /* ---- host-side parameter arithmetic (no GPU involved) ------------------------------- */

@@ -214,7 +214,7 @@ int mat_opt_in(int *sms)
     const int dev = current_device_slot();
     if (dev < 0) { set_error("imat: no current device, or its index is beyond %d", MAX_DEVICES - 1); return ICONV_ERR_UNSUPPORTED; }
     if (!done[dev].load(std::memory_order_acquire)) {
-        ICONV_CUDA_TRY(mat_opt_in_0());
+        ICONV_CUDA_TRY(mat_opt_in_0());        // (shared memory beyond 48 KB; it also has every instance loaded before a call may be captured)
         ICONV_CUDA_TRY(mat_opt_in_1());
         ICONV_CUDA_TRY(mat_opt_in_2());
         done[dev].store(1, std::memory_order_release);
@@ -243,8 +243,8 @@ int build_plan(const imat_desc &d, cudaStream_t stream, imat_plan_t *p)
     a.units = (long long)(bytes / 16); a.rows = p->ch_tiles * BLOCK_M;
     a.packed = (uint4 *)p->packed; a.row_params = p->row_params;
     const unsigned blocks = (unsigned)std::min<long long>((a.units + 255) / 256, 16ll * p->sms);
-    mat_pack_kernel<<<blocks, 256, 0, stream>>>(a);
-    ICONV_CUDA_TRY(cudaGetLastError());
+    const auto kernel = mat_pack_kernel;
+    ICONV_CUDA_TRY(launch_kernel(kernel, false, blocks, 256, 0, stream, a));
     ICONV_CUDA_TRY(cudaStreamSynchronize(stream));
     return ICONV_OK;
 }
@@ -282,12 +282,13 @@ extern "C" int imat_plan(const imat_desc *desc, void *cuda_stream, imat_plan_t *
         set_error("imat_plan: scales and biases must be 4-byte aligned");
         return ICONV_ERR_ALIGN;
     }
-    if (d.n > (1 << 24) || (long long)d.n * d.k > (1ll << 37)) { set_error("imat_plan: weights too large"); return ICONV_ERR_SHAPE; }
+    if (d.n > (1 << 24) || ((long long)d.n + 128) * (d.k + 127) * (d.up_weights ? 2 : 1) >= (1ll << 37)) { set_error("imat_plan: weights too large"); return ICONV_ERR_SHAPE; }
     imat_plan_t *p = new (std::nothrow) imat_plan_s();
     if (!p) { set_error("imat_plan: out of host memory"); return ICONV_ERR_ARG; }
     const int rc = build_plan(d, (cudaStream_t)cuda_stream, p);
     if (rc != ICONV_OK) {
         imat_plan_destroy(p);
+        cudaGetLastError();                // (an allocation that failed is reported here, not by whatever the caller launches next)
         return rc;
     }
     *plan_out = p;

@@ -285,7 +285,6 @@ __device__ __forceinline__ uint32_t mat_set_up(MatShared *sh, const MatArgs &a, 
             sh->abort_flag = 0;
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (lane == 0) grid_dep_launch();
     }
     if (warp == MMA_WARP) {
         if (PAIR) tmem_alloc_pair(smem_u32(&sh->tmem_base), (uint32_t)a.tmem_cols);
@@ -293,6 +292,7 @@ __device__ __forceinline__ uint32_t mat_set_up(MatShared *sh, const MatArgs &a, 
     }
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();     // (not before this block has its tensor memory: a block of the next kernel could take it first and wait for this kernel's end)
     if (PAIR) cluster_sync_all();                // the peer's barriers exist before anything arrives at them
     tc_fence_after();
     return sh->tmem_base;

@@ -52,11 +52,16 @@ cudaError_t ICONV_CAT(mat_launch_, ICONV_MAT_ID)(bool gated, const MatLaunch &l)
 
 cudaError_t ICONV_CAT(mat_opt_in_, ICONV_MAT_ID)()
 {
-    for (bool gated : {false, true})
+    for (bool gated : {false, true}) {
         for (MatKernel k : {instance(gated, true), instance(gated, false)}) {
             const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
             if (e != cudaSuccess) return e;
         }
+        for (bool wide : {false, true}) {
+            const cudaError_t e = cudaFuncSetAttribute(stream_instance(gated, wide), cudaFuncAttributeMaxDynamicSharedMemorySize, MAT_STREAM_SMEM);
+            if (e != cudaSuccess) return e;
+        }
+    }
     return cudaSuccess;
 }
 

@@ -20,6 +20,8 @@ constexpr int MAT_STREAM_ROWS = 32, MAT_STREAM_WARPS_MAX = 16, MAT_STREAM_TOKENS
 constexpr int MAT_STREAM_AT_ONCE = 2;            // blocks of 128 bytes of the reduction that a warp has in flight: 8 KB of weights
 constexpr int MAT_STREAM_PITCH = 36;             // words between two tokens of the sums in shared memory: the fragments' stores meet no bank twice
 
+constexpr int MAT_STREAM_SMEM = MAT_STREAM_WARPS_MAX * MAT_STREAM_TOKENS * MAT_STREAM_PITCH * 4;
+
 __device__ __forceinline__ uint4 ld_weights(const int8_t *p)      // (a plan's constants, used once: they need no place in L1)
 {
     uint4 v;
