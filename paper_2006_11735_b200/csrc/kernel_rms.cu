@@ -99,15 +99,30 @@ __device__ __forceinline__ void store_elems(T *p, const float (&f)[VE])
 // floor(v * inv + 1/2) in the low byte: both sums are rounded down, the first so that a value just under the border stays under it, the second
 // leaves the whole number beside 1.5 * 2^23 (an addition where a conversion runs at an eighth of the rate).  For |v * inv| of 127 and a rounding.
 __device__ __forceinline__ unsigned round_q(float v, float inv) { return __float_as_uint(__fadd_rd(__fadd_rd(__fmul_rn(v, inv), 0.5f), 12582912.0f)); }
+// ... of two values at a time: the same operations, two in an instruction
+__device__ __forceinline__ unsigned long long two(float a, float b)
+{
+    unsigned long long d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void round_q2(float a, float b, unsigned long long inv, unsigned &qa, unsigned &qb)
+{
+    unsigned long long t;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(two(a, b)), "l"(inv));
+    asm("add.rm.f32x2 %0, %0, %1;" : "+l"(t) : "l"(two(0.5f, 0.5f)));
+    asm("add.rm.f32x2 %0, %0, %1;" : "+l"(t) : "l"(two(12582912.0f, 12582912.0f)));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(qa), "=r"(qb) : "l"(t));
+}
 
 // inv = 0 (nothing in the row, or something that is no number): zeros
 template <int VE>
 __device__ __forceinline__ void store_q(int8_t *p, const float (&v)[VE], float inv)
 {
     unsigned b[VE];
-#pragma unroll
-    for (int j = 0; j < VE; ++j) b[j] = round_q(v[j], inv);
     if constexpr (VE > 1) {
+#pragma unroll
+        for (int j = 0; j < VE; j += 2) round_q2(v[j], v[j + 1], two(inv, inv), b[j], b[j + 1]);
 #pragma unroll
         for (int w = 0; w < VE / 4; ++w) {
             b[w] = __byte_perm(__byte_perm(b[4 * w], b[4 * w + 1], 0x0040), __byte_perm(b[4 * w + 2], b[4 * w + 3], 0x0040), 0x5410);
@@ -116,6 +131,7 @@ __device__ __forceinline__ void store_q(int8_t *p, const float (&v)[VE], float i
         if constexpr (VE == 8) *(uint2 *)p = make_uint2(b[0], b[1]);
         else *(unsigned *)p = b[0];
     } else {
+        b[0] = round_q(v[0], inv);
         *p = inv == 0.0f ? (int8_t)0 : (int8_t)b[0];
     }
 }
@@ -128,10 +144,22 @@ struct RowSums {
     __device__ __forceinline__ void squares(const float (&s)[R][VE])        // (of a thread's whole share: one look at the sum)
     {
         float p = 0.0f;
+        if constexpr (VE > 1) {
+            unsigned long long t = 0;
 #pragma unroll
-        for (int i = 0; i < R; ++i)
+            for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int j = 0; j < VE; ++j) p = fmaf(s[i][j], s[i][j], p);
+                for (int j = 0; j < VE; j += 2) {
+                    const unsigned long long e = two(s[i][j], s[i][j + 1]);
+                    asm("fma.rn.f32x2 %0, %1, %1, %0;" : "+l"(t) : "l"(e));
+                }
+            float lo, hi;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(t));
+            p = lo + hi;
+        } else {
+#pragma unroll
+            for (int i = 0; i < R; ++i) p = fmaf(s[i][0], s[i][0], p);
+        }
         sq += p;
         if (p > 1.0e25f)
 #pragma unroll
@@ -257,7 +285,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             }
         }
         if constexpr (VE > 1) {
-            m.squares(v);
+            if (a.norm) m.squares(v);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const int at = i * TPR + t;
@@ -398,7 +426,7 @@ __global__ void __launch_bounds__(32 * (STREAM_WARPS + STREAM_LOADERS), 1) rms_s
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->empty[stage]));             // the row is in registers
-            m.squares(v);
+            if (a.norm) m.squares(v);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 if (i * TPR + t < vecs) {
