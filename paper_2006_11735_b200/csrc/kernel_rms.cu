@@ -502,19 +502,22 @@ cudaError_t launch_width(const RmsArgs &a, cudaStream_t stream)
 
 using StreamKernel = void (*)(StreamArgs);
 
-// Groups that a block's warps make for rows of a width: eight of two warps, four or two, 32 elements a thread; the widest rows take 64 a thread, so that
-// two groups can still take turns (4096 rows of 16384 without a residual: 46 us, 58 in one group).
+// Groups that a block's warps make for rows of a width: eight of two warps, four or two, 32 elements a thread.  The widest rows: one group, unless
+// nothing but the row is read (`bare`); then the arithmetic is the bound and two groups of 64 elements a thread take turns (4096 rows of 16384: 42 us,
+// 58 in one group; with a residual and weights 1500 rows of 12000 take 28 us in one group, 36 in two).
 constexpr int STREAM_WIDTH_MAX = 8 * 32 * 64;
-int stream_groups(int width) { return width <= 2 * 32 * 32 ? 8 : width <= 4 * 32 * 32 ? 4 : 2; }
+int stream_groups(int width, bool bare) { return width <= 2 * 32 * 32 ? 8 : width <= 4 * 32 * 32 ? 4 : width <= 8 * 32 * 32 || bare ? 2 : 1; }
 template <typename T>
-StreamKernel stream_kernel(int width)
+StreamKernel stream_kernel(int width, bool bare)
 {
-    switch (stream_groups(width)) {
+    switch (stream_groups(width, bare)) {
     case 8: return rms_stream_kernel<T, 2, 32>;
     case 4: return rms_stream_kernel<T, 4, 32>;
-    default: return width <= 8 * 32 * 32 ? rms_stream_kernel<T, 8, 32> : rms_stream_kernel<T, 8, 64>;
+    case 2: return width <= 8 * 32 * 32 ? rms_stream_kernel<T, 8, 32> : rms_stream_kernel<T, 8, 64>;
+    default: return rms_stream_kernel<T, 16, 32>;
     }
 }
+bool bare(const RmsArgs &a) { return !a.r && !a.g; }
 
 // Shared-memory opt-in of the current device, once; its SM count.
 int stream_opt_in(int *sms)
@@ -524,8 +527,9 @@ int stream_opt_in(int *sms)
     if (dev < 0) { set_error("irms_quant: no current device, or its index is beyond %d", MAX_DEVICES - 1); return ICONV_ERR_UNSUPPORTED; }
     if (!count[dev].load(std::memory_order_acquire)) {
         for (int width = 2048; width <= STREAM_WIDTH_MAX; width *= 2)
-            for (StreamKernel k : {stream_kernel<float>(width), stream_kernel<__half>(width), stream_kernel<__nv_bfloat16>(width)})
-                ICONV_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
+            for (bool b : {false, true})
+                for (StreamKernel k : {stream_kernel<float>(width, b), stream_kernel<__half>(width, b), stream_kernel<__nv_bfloat16>(width, b)})
+                    ICONV_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
         int n = 0;
         ICONV_CUDA_TRY(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
         count[dev].store(n, std::memory_order_release);
@@ -542,7 +546,7 @@ bool streams(const RmsArgs &a, int element)
     const long long bytes = (long long)a.width * element, most = MAX_SMEM - (long long)sizeof(StreamShared);
     const bool residual = a.r != nullptr;
     return bytes >= (residual ? 16384 : 8192) && a.width <= STREAM_WIDTH_MAX && a.rows >= 4 * 148 &&
-           std::max(3, stream_groups(a.width)) * bytes * (residual ? 2 : 1) <= most;
+           std::max(3, stream_groups(a.width, bare(a))) * bytes * (residual ? 2 : 1) <= most;
 }
 
 template <typename T>
@@ -555,11 +559,11 @@ int launch_stream(const RmsArgs &a, cudaStream_t stream)
     s.a = a;
     s.row_bytes = a.width * (int)sizeof(T);
     s.stage_bytes = s.row_bytes * (a.r ? 2 : 1);
-    const int groups = stream_groups(a.width);
+    const int groups = stream_groups(a.width, bare(a));
     s.stages = std::min((MAX_SMEM - (int)sizeof(StreamShared)) / s.stage_bytes, STREAM_STAGES_MAX) / groups * groups;
     s.status = device_status_ptr();
     if (!s.status) { set_error("device status word not available"); return ICONV_ERR_CUDA; }
-    const auto kernel = stream_kernel<T>(a.width);
+    const auto kernel = stream_kernel<T>(a.width, bare(a));
     ICONV_CUDA_TRY(launch_kernel(kernel, true, (unsigned)std::min<long long>(a.rows, sms), 32 * (STREAM_WARPS + STREAM_LOADERS),
                                  (size_t)s.stages * s.stage_bytes + sizeof(StreamShared), stream, s));
     return ICONV_OK;
