@@ -326,7 +326,7 @@ ICONV_API int iconv_stem_forward_static(const istem_desc *desc, const void *x, c
 /*
  * ---- The feed-forward sublayer of a transformer in 8 bits (the paper has no counterpart; its numerics do: symmetric int8 with a
  * scale, Section 3.1, int32 sums).  A row is one token.  A matrix of rows is given by its address and its row stride in ELEMENTS; what
- * lies between a row's end and the next row is neither read nor written.
+ * lies between a row's end and the next row is not written, and what is read of it is not used.
  *
  * irms_quant -- the residual's addition, the root-mean-square norm and 8-bit rows with a scale each:
  *     s = x + residual                         in float

@@ -327,6 +327,210 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
     }
 }
 
+// ---- Rows of 16-bit elements that start anywhere (an odd width without padding): vectors of 16 bytes all the same (2000 rows of 16001 with a
+// residual: 92 us, 367 element by element; 8192 of 4001 alone 44 and 80; in float single elements are as fast: 82 us, 124 so).  A thread's VE elements lie across two aligned 16-byte
+// words; both are loaded (the second is the neighbour's first, and in L1) and shifted by the row's phase, which is the same for all its threads.
+// The sum goes back the other way: a lane stores the aligned word that its own elements and the lane's before it make up, and the ends of a
+// warp's stretch go out element by element.  q's rows are aligned.
+
+// Bytes off ... off + 15 of the 32 that a and b make.
+__device__ __forceinline__ uint4 cut16(const uint4 &a, const uint4 &b, unsigned off)
+{
+    const unsigned bits = (off & 3u) * 8u;
+    uint4 d;
+    switch (off >> 2) {
+    case 0:
+        d.x = __funnelshift_r(a.x, a.y, bits); d.y = __funnelshift_r(a.y, a.z, bits); d.z = __funnelshift_r(a.z, a.w, bits); d.w = __funnelshift_r(a.w, b.x, bits);
+        break;
+    case 1:
+        d.x = __funnelshift_r(a.y, a.z, bits); d.y = __funnelshift_r(a.z, a.w, bits); d.z = __funnelshift_r(a.w, b.x, bits); d.w = __funnelshift_r(b.x, b.y, bits);
+        break;
+    case 2:
+        d.x = __funnelshift_r(a.z, a.w, bits); d.y = __funnelshift_r(a.w, b.x, bits); d.z = __funnelshift_r(b.x, b.y, bits); d.w = __funnelshift_r(b.y, b.z, bits);
+        break;
+    default:
+        d.x = __funnelshift_r(a.w, b.x, bits); d.y = __funnelshift_r(b.x, b.y, bits); d.z = __funnelshift_r(b.y, b.z, bits); d.w = __funnelshift_r(b.z, b.w, bits);
+        break;
+    }
+    return d;
+}
+
+// A matrix to be read so: its first and last 16-byte words that lie in it whole.
+struct Window {
+    const char *first, *last;
+};
+// The two words around a vector; near the matrix's ends other ones of it instead (exact: those were the right ones).
+struct Pair {
+    uint4 a, b;
+    bool exact;
+};
+__device__ __forceinline__ Pair load_pair(const char *at, const Window &w)
+{
+    const char *base = at - ((uintptr_t)at & 15);
+    const char *from = base < w.first ? w.first : base + 16 > w.last ? w.last - 16 : base;
+    Pair p;
+    p.a = ld_tensor((const uint4 *)from);
+    p.b = ld_tensor((const uint4 *)from + 1);
+    p.exact = from == base;
+    return p;
+}
+// ... as numbers; `count` of them are the row's
+template <typename T, int VE>
+__device__ __forceinline__ void pair_to_float(const Pair &p, const char *at, int count, float (&f)[VE])
+{
+    if (p.exact) {
+        Raw<T, VE> v;
+        v.w = cut16(p.a, p.b, (unsigned)(uintptr_t)at & 15u);
+        to_float<T, VE>(v, f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) f[j] = j < count ? Elem<T>::to(((const T *)at)[j]) : 0.0f;
+    }
+    if (count < VE)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) f[j] = j < count ? f[j] : 0.0f;
+}
+// A warp's vectors to consecutive places from its first lane's `at` on; all lanes take part.  count: this lane's elements (VE, fewer in the row's last
+// vector, or none).
+template <typename T, int VE>
+__device__ __forceinline__ void store_shifted(T *at, const float (&f)[VE], int count, int lane)
+{
+    union { T e[VE]; uint4 w; } o;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) o.e[j] = Elem<T>::from(f[j]);
+    const unsigned off = (unsigned)(uintptr_t)at & 15u;                      // the same in every lane
+    const unsigned whole = __ballot_sync(0xffffffffu, count == VE);          // the first lanes
+    int from = 0, to = 0;                                                    // elements that go out one by one
+    if (off == 0) {
+        if (count == VE) *(uint4 *)at = o.w;
+    } else {
+        uint4 before;
+        before.x = __shfl_up_sync(0xffffffffu, o.w.x, 1); before.y = __shfl_up_sync(0xffffffffu, o.w.y, 1);
+        before.z = __shfl_up_sync(0xffffffffu, o.w.z, 1); before.w = __shfl_up_sync(0xffffffffu, o.w.w, 1);
+        if (count == VE && lane > 0) *(uint4 *)((char *)at - off) = cut16(before, o.w, 16u - off);
+        if (count == VE && lane == 0) to = VE - (int)(off / sizeof(T));
+        if (lane == __popc(whole) - 1) {                                     // what the lane behind would have taken along
+            if (lane > 0) from = VE - (int)(off / sizeof(T));
+            to = VE;
+        }
+    }
+    if (count < VE) to = count;
+    if (to > from)
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            if (j >= from && j < to) at[j] = o.e[j];
+}
+
+struct ShiftArgs {
+    RmsArgs a;
+    Window x, r, g;
+};
+
+template <typename T, int TPR, int R>
+__global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_shift_kernel(const __grid_constant__ ShiftArgs s)
+{
+    constexpr int VE = 16 / (int)sizeof(T), ROWS = TPR > 128 ? 1 : 128 / TPR;
+    __shared__ RowSums sh[ROW_WARPS_MAX];
+    const RmsArgs &a = s.a;
+    grid_dep_launch();
+    grid_dep_wait();
+    const int lane = threadIdx.x & 31, t = ROWS > 1 ? lane : (int)threadIdx.x;
+    const long long row = (long long)blockIdx.x * ROWS + (ROWS > 1 ? (int)(threadIdx.x >> 5) : 0);
+    if (row >= a.rows) return;
+    const char *x = (const char *)((const T *)a.x + row * a.ldx), *r = a.r ? (const char *)((const T *)a.r + row * a.ldr) : nullptr;
+    T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
+    int8_t *q = a.q + row * a.ldq;
+    const bool g_pairs = a.g && !a.g_f32;
+    RowSums m = {0.0f, 0.0f, 0.0f};
+    float v[R][VE];
+    Pair xp[R], rp[R], gp[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int byte = (i * TPR + t) * 16;
+        xp[i] = load_pair(x + byte, s.x);
+        if (r) rp[i] = load_pair(r + byte, s.r);
+        if (g_pairs) gp[i] = load_pair((const char *)a.g + byte, s.g);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int at = (i * TPR + t) * VE, left = a.width - at, count = left < 0 ? 0 : left < VE ? left : VE;
+        pair_to_float<T, VE>(xp[i], x + at * (int)sizeof(T), count, v[i]);
+        if (r) {
+            float o[VE];
+            pair_to_float<T, VE>(rp[i], r + at * (int)sizeof(T), count, o);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[i][j] = __fadd_rn(v[i][j], o[j]);
+        }
+        if (out) store_shifted<T, VE>(out + at, v[i], count, lane);
+    }
+    if (a.norm) m.squares(v);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int at = (i * TPR + t) * VE, left = a.width - at, count = left < 0 ? 0 : left < VE ? left : VE;
+        if (g_pairs) {
+            float g[VE];
+            pair_to_float<T, VE>(gp[i], (const char *)((const T *)a.g + at), count, g);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[i][j] = __fmul_rn(v[i][j], g[j]);
+        } else if (a.g) {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[i][j] = j < count ? __fmul_rn(v[i][j], ((const float *)a.g)[at + j]) : 0.0f;
+        }
+        m.largest(v[i]);
+    }
+    row_reduce<TPR>(m, sh);
+    const float inv = finish_row(a, m, row, t == 0);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int at = (i * TPR + t) * VE, count = a.width - at;
+        if (count >= VE) {
+            store_q<VE>(q + at, v[i], inv);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                if (j < count) q[at + j] = inv == 0.0f ? (int8_t)0 : (int8_t)round_q(v[i][j], inv);
+        }
+    }
+}
+
+template <typename T, int TPR, int R>
+cudaError_t launch_shift_one(const ShiftArgs &s, cudaStream_t stream)
+{
+    constexpr int ROWS = TPR > 128 ? 1 : 128 / TPR;
+    const auto kernel = rms_shift_kernel<T, TPR, R>;
+    return launch_kernel(kernel, true, (unsigned)((s.a.rows + ROWS - 1) / ROWS), TPR > 128 ? TPR : 128, 0, stream, s);
+}
+constexpr int SHIFT_VECTORS_MAX = 2048;
+
+// Where a matrix has no two whole words to read there is nothing to gain.
+bool window_of(const void *p, long long rows, long long stride, int width, int element, Window &w)
+{
+    const char *begin = (const char *)p, *end = begin + ((rows - 1) * stride + width) * element;
+    w.first = begin + (16 - (uintptr_t)begin % 16) % 16;
+    w.last = end - (uintptr_t)end % 16 - 16;
+    return w.last >= w.first + 16;
+}
+template <typename T>
+bool shift_args(const RmsArgs &a, ShiftArgs &s)
+{
+    constexpr int VE = 16 / (int)sizeof(T), E = (int)sizeof(T);
+    s.a = a;
+    return !((uintptr_t)a.q % VE) && !(a.ldq % VE) && (a.width + VE - 1) / VE <= SHIFT_VECTORS_MAX && window_of(a.x, a.rows, a.ldx, a.width, E, s.x) &&
+           (!a.r || window_of(a.r, a.rows, a.ldr, a.width, E, s.r)) && (!a.g || a.g_f32 || window_of(a.g, 1, a.width, a.width, E, s.g));
+}
+template <typename T>
+cudaError_t launch_shift(const ShiftArgs &s, cudaStream_t stream)
+{
+    const int vecs = (s.a.width + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T));
+    if (vecs <= 32) return launch_shift_one<T, 32, 1>(s, stream);
+    if (vecs <= 64) return launch_shift_one<T, 32, 2>(s, stream);
+    if (vecs <= 128) return launch_shift_one<T, 128, 1>(s, stream);
+    if (vecs <= 256) return launch_shift_one<T, 128, 2>(s, stream);
+    if (vecs <= 512) return launch_shift_one<T, 256, 2>(s, stream);
+    if (vecs <= 1024) return launch_shift_one<T, 512, 2>(s, stream);
+    return launch_shift_one<T, 512, 4>(s, stream);
+}
+
 // Many wide rows: one block per SM, whose loading warps keep a ring of whole rows in shared memory ahead of the arithmetic, so that the memory
 // stays busy while a row is being reduced (a block per row has nothing in flight then: 4096 rows of 16384 in bfloat16 took 86 us, 46 this
 // way, floor 31).  Groups of GW warps take the rows in turn, ELEMS elements a thread; a group meets at one named barrier per row.  The ring's stages
@@ -574,6 +778,13 @@ int launch_rms(const RmsArgs &a, bool whole, cudaStream_t stream)
 {
     constexpr int VE = 16 / (int)sizeof(T);
     if (whole && streams(a, (int)sizeof(T))) return launch_stream<T>(a, stream);
+    if constexpr (sizeof(T) == 2) {
+        ShiftArgs s;
+        if (!whole && shift_args<T>(a, s)) {
+            ICONV_CUDA_TRY(launch_shift<T>(s, stream));
+            return ICONV_OK;
+        }
+    }
     ICONV_CUDA_TRY((whole ? launch_width<T, VE>(a, stream) : launch_width<T, 1>(a, stream)));
     return ICONV_OK;
 }

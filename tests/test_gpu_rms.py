@@ -187,3 +187,61 @@ def test_many_wide_rows_in_place_and_with_strides():
         q, scales, total = rms_call(into if first else x, r if first else into, g, q=q_store[:, :d], total=into)
         assert torch.equal(q, want[0]) and torch.equal(scales, want[1]) and torch.equal(total, want[2]) and (q_store[:, d:] == 77).all()
     B.iconv_check(stream())
+
+
+def _anywhere(gen, m, d, stride, first, dtype):
+    """A matrix whose first element is `first` elements into its memory, and the memory."""
+    store = torch.randn(first + m * stride + 8, generator=gen, device="cuda").to(TYPES[dtype])
+    return store.as_strided((m, d), (stride, 1), first), store
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [9, 31, 33, 63, 100, 255, 257, 500, 511, 513, 1001, 2047, 2049, 4001, 4100, 8191, 16383, 16385])
+def test_rows_that_start_anywhere(dtype, d):
+    """Vectors cut out of aligned words: every phase of x, the residual, the sum and the weights, q in aligned rows, first and last rows of
+    their memory; what lies around the rows stays."""
+    gen = generator(d)
+    for case, (px, pr, ps, fx, fr, fs, fg) in enumerate([(0, 0, 0, 0, 0, 0, 0), (1, 0, 3, 1, 2, 3, 5), (7, 2, 1, 5, 0, 7, 1), (0, 5, 8, 3, 3, 0, 2)]):
+        for m in (1, 3, 10):
+            x, _ = _anywhere(gen, m, d, d + px, fx, dtype)
+            r, _ = _anywhere(gen, m, d, d + pr, fr, dtype)
+            g = torch.randn(d + 8, generator=gen, device="cuda").to(TYPES[dtype])[fg:fg + d] if case != 2 else 1 + torch.rand(d, generator=gen, device="cuda")
+            total, store = _anywhere(gen, m, d, d + ps, fs, dtype)
+            before = store.clone()
+            q_store = torch.full((m + 1, -(-d // 16) * 16 + 16), 77, dtype=torch.int8, device="cuda")
+            q, scales, _ = rms_call(x, r, g, q=q_store[:m, :d], total=total)
+            rms_check(x, r, g, q, scales, total)
+            assert (q_store[:, d:] == 77).all() and (q_store[m] == 77).all()
+            inside = torch.zeros_like(store, dtype=torch.bool)
+            inside.as_strided((m, d), (d + ps, 1), fs).fill_(True)
+            assert torch.equal(store[~inside], before[~inside])
+            q, scales, _ = rms_call(x, norm=0, with_sum=False, q=q_store[:m, :d])
+            rms_check(x, None, None, q, scales, None, norm=0)
+    B.iconv_check(stream())
+
+
+@pytest.mark.parametrize("into", ["x", "r"])
+@pytest.mark.parametrize("d", [513, 2049, 4001])
+def test_rows_that_start_anywhere_in_place(d, into):
+    gen = generator(d)
+    x, r = (_anywhere(gen, 300, d, d, first, "bf16")[0] for first in (0, 3))
+    g = torch.randn(d, generator=gen, device="cuda").bfloat16()
+    q = lambda: torch.empty(300, -(-d // 16) * 16, dtype=torch.int8, device="cuda")[:, :d]
+    want = rms_call(x, r, g, q=q())
+    x2, r2 = (torch.empty(300 * d + 3, dtype=torch.bfloat16, device="cuda").as_strided((300, d), (d, 1), first).copy_(t) for first, t in ((0, x), (3, r)))
+    q2, scales, total = rms_call(x2, r2, g, q=q(), total=x2 if into == "x" else r2)
+    assert torch.equal(q2, want[0]) and torch.equal(scales, want[1]) and torch.equal(total, want[2])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_bad_values_beside_a_row_do_not_reach_it(dtype):
+    """What a vector's words hold besides its own elements: NaN in the rows before and behind, and between rows."""
+    m, d, stride = 7, 517, 521
+    x, store = _anywhere(generator(5), m, d, stride, 1, dtype)
+    clean = rms_call(x.clone(), q=torch.empty(m, 528, dtype=torch.int8, device="cuda")[:, :d])
+    keep = torch.zeros_like(store, dtype=torch.bool)
+    keep.as_strided((m, d), (stride, 1), 1)[::2].fill_(True)
+    store[~keep] = float("nan")
+    q, scales, total = rms_call(x, q=torch.empty(m, 528, dtype=torch.int8, device="cuda")[:, :d])
+    assert torch.equal(q[::2], clean[0][::2]) and torch.equal(total[::2], clean[2][::2]) and torch.isnan(scales[1::2]).all()
+    assert ((scales - clean[1]).abs()[::2] <= 40 * 2.0 ** -24 * scales[::2]).all()
