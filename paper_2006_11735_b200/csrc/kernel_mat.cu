@@ -130,6 +130,10 @@ MatChoice choice_stream(const imat_plan_t *p, long long rows)
 // 110 drawn sizes its choice took 3 % longer than the best of all forms on average (geometric mean), 33 % at most.
 constexpr double SM_RATE = 87.0, HBM_RATE = 6300.0, ROUND_LATENCY = 1100.0, ISSUE = 190.0;
 
+// Up to here a few tokens stream.  The streaming kernel's blocks fill the SM's registers, so that nothing of the kernel behind comes up beside them: among
+// other kernels a call with 17 MB of weights takes 4.9 us so and 5.4 on the few-tile kernel, one with 34 MB 9.9 and 7.3, one with 67 MB 18.6 and 12.0.
+constexpr double MAT_STREAM_BYTES = 24.0 * 1048576.0;
+
 struct CallShape {
     long long rows;
     double weight_bytes, hbm;              // bytes of weights; nanoseconds that the call's bytes take from HBM
@@ -187,7 +191,7 @@ MatChoice choose(const imat_plan_t *p, long long rows, bool residual)
     auto offer = [&](const MatChoice &c, double cost) {
         if (c.smem <= (size_t)MAX_SMEM && (least < 0.0 || cost < least)) { least = cost; best = c; }
     };
-    if (rows <= MAT_STREAM_TOKENS) {
+    if (rows <= MAT_STREAM_TOKENS && s.weight_bytes <= MAT_STREAM_BYTES) {
         const MatChoice c = choice_stream(p, rows);
         offer(c, cost_stream(p, s, c));
     }
