@@ -152,13 +152,10 @@ __device__ __forceinline__ void mat_load_residual(const MatArgs &a, long long to
         r += j < last ? a.ld_res : 0;
     }
 }
-// WHOLE: every token exists, and every lane's channel.
-template <typename T, bool GATED, int P, bool WHOLE>
-__device__ __forceinline__ void mat_finish(const MatArgs &a, const int (&acc)[P], const float (&sx)[P], const T (&res)[P], long long tok, int ch, float2 par, int lane)
+// What the lane stores, from the sums: y[j] of token tok + j, or, gated, of token tok + 2 j + (lane >= 16) for j < P / 2.
+template <typename T, bool GATED, int P>
+__device__ __forceinline__ void mat_values(const MatArgs &a, const int (&acc)[P], const float (&sx)[P], const T (&res)[P], float2 par, int lane, float (&y)[P])
 {
-    const int count = WHOLE ? P : ch < a.n ? (int)(a.m - tok < P ? a.m - tok : P) : 0;       // tokens that this lane stores
-    T *out = (T *)a.out + tok * a.ld_out + ch;
-    float y[P];
 #pragma unroll
     for (int j = 0; j < P; ++j) y[j] = fmaf((float)acc[j] * par.x, sx[j], par.y);
     if (!GATED) {
@@ -166,11 +163,6 @@ __device__ __forceinline__ void mat_finish(const MatArgs &a, const int (&acc)[P]
         if (a.residual)
 #pragma unroll
             for (int j = 0; j < P; ++j) y[j] += mat_value<T>(res[j]);
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-            if (WHOLE || j < count) *out = mat_round<T>(y[j]);
-            out += a.ld_out;                // (a product per store, behind its predicate, took twice as long)
-        }
     } else {
         // lanes 0-15 hold the gate of 16 channels, lanes 16-31 their up projection: of two tokens the lower lanes finish the first, the upper ones the second
         const bool up_lane = lane >= 16;
@@ -182,12 +174,22 @@ __device__ __forceinline__ void mat_finish(const MatArgs &a, const int (&acc)[P]
             u[p] = up_lane ? y[2 * p + 1] : other;
         }
         mat_act<P / 2>(a.act, g);
-        out += up_lane ? a.ld_out : 0;
 #pragma unroll
-        for (int p = 0; p < P / 2; ++p) {
-            if (WHOLE || 2 * p + (up_lane ? 1 : 0) < count) *out = mat_round<T>(g[p] * u[p]);
-            out += 2 * a.ld_out;
-        }
+        for (int p = 0; p < P / 2; ++p) y[p] = g[p] * u[p];
+    }
+}
+// WHOLE: every token exists, and every lane's channel.
+template <typename T, bool GATED, int P, bool WHOLE>
+__device__ __forceinline__ void mat_store(const MatArgs &a, const float (&y)[P], long long tok, int ch, int lane)
+{
+    const int count = WHOLE ? P : ch < a.n ? (int)(a.m - tok < P ? a.m - tok : P) : 0;       // tokens that this lane stores
+    const int first = GATED && lane >= 16 ? 1 : 0;
+    T *out = (T *)a.out + (tok + first) * a.ld_out + ch;
+    const long long step = GATED ? 2 * a.ld_out : a.ld_out;
+#pragma unroll
+    for (int j = 0; j < (GATED ? P / 2 : P); ++j) {
+        if (WHOLE || (GATED ? 2 * j + first : j) < count) *out = mat_round<T>(y[j]);
+        out += step;                        // (a product per store, behind its predicate, took twice as long)
     }
 }
 
@@ -202,10 +204,9 @@ __device__ __forceinline__ void mat_tmem_ld8(uint32_t taddr, int (&r)[8])
 }
 
 // A warp's share of a tile's epilogue: columns P part ... of every P `parts`.  What the next group reads is asked for before this one is
-// finished; the first group's is in hand (`begin`) while the accumulators are still being summed up.
-template <typename T, bool GATED>
+// stored, in the registers that it has just given free; the first group's is in hand (`begin`) while the accumulators are still being summed up.
+template <typename T, bool GATED, int P>
 struct MatColumns {
-    static constexpr int P = 8;
     float sx[P];
     T res[P];
     __device__ __forceinline__ void load(const MatArgs &a, long long tok, int ch)
@@ -219,15 +220,17 @@ struct MatColumns {
     }
     __device__ __forceinline__ void run(const MatArgs &a, uint32_t t_row, long long tok_first, int columns, int ch, float2 par, int part, int parts, int lane)
     {
+        const bool all = P == 16 && __all_sync(0xffffffffu, ch < a.n);
 #pragma unroll 1
         for (int c = part * P; c < columns; c += parts * P) {
             int acc[P];
-            mat_tmem_ld8(t_row + (uint32_t)c, acc);
-            MatColumns next;
-            const bool more = c + parts * P < columns;
-            if (more) next.load(a, tok_first + c + parts * P, ch);
-            mat_finish<T, GATED, P, false>(a, acc, sx, res, tok_first + c, ch, par, lane);
-            if (more) *this = next;
+            float y[P];
+            if constexpr (P == 8) mat_tmem_ld8(t_row + (uint32_t)c, acc);
+            else tmem_ld16_sync(t_row + (uint32_t)c, acc);
+            mat_values<T, GATED, P>(a, acc, sx, res, par, lane, y);
+            if (c + parts * P < columns) load(a, tok_first + c + parts * P, ch);
+            if (P == 16 && all && c + P <= columns) mat_store<T, GATED, P, true>(a, y, tok_first + c, ch, lane);
+            else mat_store<T, GATED, P, false>(a, y, tok_first + c, ch, lane);
         }
     }
 };
@@ -241,24 +244,6 @@ __device__ __forceinline__ void mat_prefetch_residual(const MatArgs &a, long lon
     for (int c = part * P; c < columns; c += parts * P)
         if (lane < P && c + lane < columns)
             asm volatile("prefetch.global.L2 [%0];" ::"l"((const T *)a.residual + (tok_first + c + lane) * a.ld_res + ch_first));
-}
-
-// The same in the bulk kernel, 16 columns at a time as they come: with sixteen warps the others cover what one waits for, and the registers
-// for two groups would not fit (4096 x 4096 x 4096 with a residual: 49 us, 69 with the next group's values in flight).
-template <typename T, bool GATED>
-__device__ __forceinline__ void mat_columns_bulk(const MatArgs &a, uint32_t t_row, long long tok_first, int columns, int ch, float2 par, int part, int parts, int lane)
-{
-    const bool all = __all_sync(0xffffffffu, ch < a.n) != 0;
-    for (int c = part * 16; c < columns; c += parts * 16) {
-        float sx[16];
-        T res[16];
-        int acc[16];
-        mat_load_scales<16>(a, tok_first + c, sx);
-        if (!GATED && a.residual) mat_load_residual<T, 16>(a, tok_first + c, ch, res);
-        tmem_ld16_sync(t_row + (uint32_t)c, acc);
-        if (all && c + 16 <= columns) mat_finish<T, GATED, 16, true>(a, acc, sx, res, tok_first + c, ch, par, lane);
-        else mat_finish<T, GATED, 16, false>(a, acc, sx, res, tok_first + c, ch, par, lane);
-    }
 }
 
 // What both kernels set up; `consumers` epilogue warps give an accumulator back.  Warp 0 does the barriers, a lane each, and arms
@@ -433,13 +418,15 @@ mat_bulk_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constan
             const long long tok_first = (long long)tt * a.nt;
             const int columns = a.m - tok_first < a.nt ? (int)(a.m - tok_first) : a.nt;
             if (!GATED) mat_prefetch_residual<T, 16>(a, tok_first, columns, ct * BLOCK_M + quad * 32, part, MAT_BULK_EPI / 4, lane);
+            MatColumns<T, GATED, 16> share;
+            share.begin(a, tok_first, columns, ch, part);
             if (!mbar_wait_warp(smem_u32(&sh->tmem_full[buf]), (uint32_t)((t >> 1) & 1), &sh->abort_flag, lane)) {
                 mat_give_up(sh, a.status, 4);
                 break;
             }
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * MAT_BULK_TOKENS);
-            mat_columns_bulk<T, GATED>(a, t_row, tok_first, columns, ch, par, part, MAT_BULK_EPI / 4, lane);
+            share.run(a, t_row, tok_first, columns, ch, par, part, MAT_BULK_EPI / 4, lane);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_leader(smem_u32(&sh->tmem_empty[buf]));
@@ -566,12 +553,12 @@ __device__ __forceinline__ void mat_reduce(const MatArgs &a, MatShared *sh, cons
             acc0[0] += (int)o.x; acc0[1] += (int)o.y; acc0[2] += (int)o.z; acc0[3] += (int)o.w;
             acc1[0] += (int)q.x; acc1[1] += (int)q.y; acc1[2] += (int)q.z; acc1[3] += (int)q.w;
         }
-        MatPieces<T, GATED> next;
-        const bool more = j + 4 < p.owned;
-        if (more) next.load(a, p, tok_first, j + 4, ch);
-        mat_finish<T, GATED, 4, false>(a, acc0, in.sx0, in.res0, tok0, ch, par, lane);
-        if (two) mat_finish<T, GATED, 4, false>(a, acc1, in.sx1, in.res1, tok1, ch, par, lane);
-        if (more) in = next;
+        float y0[4], y1[4];
+        mat_values<T, GATED, 4>(a, acc0, in.sx0, in.res0, par, lane, y0);
+        mat_values<T, GATED, 4>(a, acc1, in.sx1, in.res1, par, lane, y1);
+        if (j + 4 < p.owned) in.load(a, p, tok_first, j + 4, ch);
+        mat_store<T, GATED, 4, false>(a, y0, tok0, ch, lane);
+        if (two) mat_store<T, GATED, 4, false>(a, y1, tok1, ch, lane);
     }
 }
 
@@ -658,7 +645,7 @@ mat_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         const int ch = mat_channel<GATED>(ct, quad, lane);
         const float2 par = __ldg(a.row_params + (size_t)ct * BLOCK_M + quad * 32 + lane);
         const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16);
-        MatColumns<T, GATED> share;
+        MatColumns<T, GATED, 8> share;
         MatPieces<T, GATED> pieces;
         if (!GATED && a.split == 1) mat_prefetch_residual<T, 8>(a, tok_first, columns, ct * BLOCK_M + quad * 32, part, MAT_FEW_EPI / 4, lane);
         if (a.split == 1) share.begin(a, tok_first, columns, ch, part);
