@@ -18,8 +18,9 @@
 //                     each other their int32 parts through distributed shared memory (whole numbers: the order does not matter,
 //                     nothing is kept in global memory, two calls share nothing).
 //
-// In both a warp loads the weights (before it waits for the kernel ahead in the stream: they are constants), another the rows, a third
-// issues the instructions, eight or sixteen run the epilogue.  All waits are bounded as in the convolution kernels.
+// In both a warp loads the weights, another the rows, a third issues the instructions, eight or sixteen run the epilogue.  The first round of
+// weights is asked for before the wait for the kernel ahead in the stream (they are constants); nobody starts a bounded wait before that one is
+// over, however long the kernel ahead takes.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -43,7 +44,7 @@ struct MatArgs {
     int nt;                         // tokens of a tile
     int k_blocks;                   // 128-byte blocks of the reduction
     int stages, stage_bytes;
-    int split, recv_bytes;          // few-token kernel: parts of a tile's reduction; memory for the sums that other parts send
+    int split, recv_bytes;          // few-tile kernel: parts of a tile's reduction; memory for the sums that other parts send
     int tmem_cols;
     unsigned idesc;
     int act;
@@ -363,6 +364,7 @@ mat_bulk_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constan
                     const uint32_t full = smem_u32(&sh->full[stage]);
                     const uint32_t dst = smem_u32(tiles + (size_t)stage * a.stage_bytes);
                     if (!armed) {
+                        grid_dep_wait();
                         if (!mbar_wait(smem_u32(&sh->empty[stage]), parity ^ 1u, &sh->abort_flag)) {
                             mat_give_up(sh, a.status, 1);
                             ok = false;
@@ -381,6 +383,7 @@ mat_bulk_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constan
         __syncwarp();
     } else if (warp == MMA_WARP) {
         // ---------------------------------------------------------------- MMA issuer
+        grid_dep_wait();
         if (rank == 0) {
             const uint32_t a_lo0 = ((smem_u32(tiles) & 0x3FFFFu) >> 4) | (1u << 16);
             IssueRing ring;
@@ -596,7 +599,7 @@ mat_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     if (warp < 2) {
         // ---------------------------------------------------------------- loaders: warp 0 the weights, warp 1 the rows (from the second round on)
         if (lane == 0) {
-            if (warp == 1) grid_dep_wait();                     // the rows may come from the kernel before this one
+            grid_dep_wait();                     // the rows may come from the kernel before this one
             const uint32_t bytes = (uint32_t)(warp == 0 ? MAT_BLOCK : a.nt * 128);
             int stage = 0;
             uint32_t parity = 1;
@@ -618,6 +621,7 @@ mat_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         if (!alone) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     } else if (warp == MMA_WARP) {
         // ---------------------------------------------------------------- MMA issuer
+        grid_dep_wait();
         const uint32_t a_lo0 = ((smem_u32(tiles) & 0x3FFFFu) >> 4) | (1u << 16);
         IssueRing ring;
         ring.stage = 0; ring.parity = 0; ring.a_lo = a_lo0;
