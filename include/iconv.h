@@ -342,7 +342,7 @@ ICONV_API int iconv_stem_forward_static(const istem_desc *desc, const void *x, c
  *   sum           DEVICE rows x width of dtype, or NULL: not written; may be x or residual itself, at the same stride
  *   q             DEVICE int8 rows x width; scales DEVICE float [rows]
  * Addresses are aligned to their element (16-byte aligned ones, and a width and strides in multiples of 16 bytes -- 8
- * for q, 4 with ICONV_F32 -- are the fast form).  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
+ * for q, 4 with ICONV_F32 -- are the fast form).  width is at most 2^24.  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
  */
 typedef struct {
     int64_t rows;
@@ -367,7 +367,7 @@ ICONV_API int irms_quant(const irms_desc *desc, const void *x, const void *resid
  *
  * imat_plan copies the weights into a layout of its own, n * k bytes (twice that when gated) rounded up to blocks of 128 x 128, with
  * cudaMalloc on the current device; what desc points to may go afterwards.  It enqueues on cuda_stream and waits for it: call it outside any
- * stream capture, on the stream that wrote the weights.  ICONV_ERR_OVERFLOW when k reaches 131072 (the sums would not fit
+ * stream capture (inside one it is refused), on the stream that wrote the weights.  ICONV_ERR_OVERFLOW when k reaches 131072 (the sums would not fit
  * int32 whatever the values).
  * imat_forward: a plan belongs to its device, which must be current.  It enqueues one kernel, needs no workspace and keeps nothing: calls of
  * one plan may overlap on any streams and may be captured.

@@ -287,6 +287,11 @@ extern "C" int imat_plan(const imat_desc *desc, void *cuda_stream, imat_plan_t *
         return ICONV_ERR_ALIGN;
     }
     if (d.n > (1 << 24) || ((long long)d.n + 128) * (d.k + 127) * (d.up_weights ? 2 : 1) >= (1ll << 37)) { set_error("imat_plan: weights too large"); return ICONV_ERR_SHAPE; }
+    if (d.w_stride > (1ll << 46) / d.n) { set_error("imat_plan: w_stride too large"); return ICONV_ERR_SHAPE; }
+    // (an allocation or a wait would end a capture)
+    cudaStreamCaptureStatus capture;
+    ICONV_CUDA_TRY(cudaStreamIsCapturing((cudaStream_t)cuda_stream, &capture));
+    if (capture != cudaStreamCaptureStatusNone) { set_error("imat_plan: the stream is capturing"); return ICONV_ERR_CUDA; }
     imat_plan_t *p = new (std::nothrow) imat_plan_s();
     if (!p) { set_error("imat_plan: out of host memory"); return ICONV_ERR_ARG; }
     const int rc = build_plan(d, (cudaStream_t)cuda_stream, p);

@@ -35,6 +35,8 @@ struct RmsArgs {
 constexpr int ROW_WARPS_MAX = 32;
 constexpr float TINY_ROW = 1.504632769052528e-36f;  // 2^-119: 127 / a is finite from here on
 constexpr float DOWN = 7.888609052210118e-31f;      // 2^-100
+constexpr float UP = 1.2379400392853803e+27f;       // 2^90
+constexpr float MUCH = 1.0e25f, LITTLE = 1.0e-18f;  // sums of squares beyond which others are kept besides
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -136,37 +138,9 @@ __device__ __forceinline__ void store_q(int8_t *p, const float (&v)[VE], float i
     }
 }
 
-// What a row's threads gather: the sum of squares; the same of the values 2^-100 of themselves, for the case that the other does not fit, over the
-// threads whose squares pass 1e25 (what the others hold is nothing beside a sum that does not fit); the largest magnitude.
+// What a row's threads gather: the sum of squares and the largest magnitude.
 struct RowSums {
-    float sq, sq_down, top;
-    template <int R, int VE>
-    __device__ __forceinline__ void squares(const float (&s)[R][VE])        // (of a thread's whole share: one look at the sum)
-    {
-        float p = 0.0f;
-        if constexpr (VE > 1) {
-            unsigned long long t = 0;
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int j = 0; j < VE; j += 2) {
-                    const unsigned long long e = two(s[i][j], s[i][j + 1]);
-                    asm("fma.rn.f32x2 %0, %1, %1, %0;" : "+l"(t) : "l"(e));
-                }
-            float lo, hi;
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(t));
-            p = lo + hi;
-        } else {
-#pragma unroll
-            for (int i = 0; i < R; ++i) p = fmaf(s[i][0], s[i][0], p);
-        }
-        sq += p;
-        if (p > 1.0e25f)
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int j = 0; j < VE; ++j) sq_down = fmaf(s[i][j] * DOWN, s[i][j] * DOWN, sq_down);
-    }
+    float sq, top;
     template <int VE>
     __device__ __forceinline__ void largest(const float (&v)[VE])
     {
@@ -176,18 +150,65 @@ struct RowSums {
     __device__ __forceinline__ void join(const RowSums &o)
     {
         sq += o.sq;
-        sq_down += o.sq_down;
         top = max_nan(top, o.top);
     }
 };
+
+// The far sum, for a row whose sum of squares is too large or too small for a float: of the values 2^-100 of themselves where a thread's
+// squares pass MUCH (what other threads hold is nothing beside a sum that does not fit), or, as a negative number, of the values 2^90 of themselves where
+// they stay under LITTLE and eps does not cover them.
+template <int R, int VE>
+__device__ __forceinline__ void add_far(const float (&s)[R][VE], bool much, float &far)
+{
+    const float by = much ? DOWN : UP;
+    float f = 0.0f;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) f = fmaf(s[i][j] * by, s[i][j] * by, f);
+    far += much ? f : -f;
+}
+// Squares of a thread's whole share of a row.
+template <int R, int VE>
+__device__ __forceinline__ float squares(const float (&s)[R][VE])
+{
+    if constexpr (VE > 1) {
+        unsigned long long t = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < VE; j += 2) {
+                const unsigned long long e = two(s[i][j], s[i][j + 1]);
+                asm("fma.rn.f32x2 %0, %1, %1, %0;" : "+l"(t) : "l"(e));
+            }
+        float lo, hi;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(t));
+        return lo + hi;
+    } else {
+        float p = 0.0f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) p = fmaf(s[i][0], s[i][0], p);
+        return p;
+    }
+}
+// ... and the far sum with it, where s is gone when the row's sum is known
+template <int R, int VE>
+__device__ __forceinline__ float squares_and_far(const float (&s)[R][VE], float eps, float &far)
+{
+    const float p = squares(s);
+    if (p > MUCH || (eps < LITTLE && p < LITTLE)) add_far(s, p > MUCH, far);
+    return p;
+}
+// Whether the far sums decide, and a thread's part of them.
+__device__ __forceinline__ bool far_decides(const RmsArgs &a, const RowSums &m) { return a.norm && (!(m.sq <= FLT_MAX) || (m.sq < LITTLE && a.eps < LITTLE)); }
+__device__ __forceinline__ float far_part(const RowSums &m, float far) { return m.sq < LITTLE ? -far : fmaxf(far, 0.0f); }
 
 // Over the TPR threads of a row (a warp's, or the whole block's); every thread gets the result.
 template <int TPR>
 __device__ __forceinline__ void row_reduce(RowSums &m, RowSums *sh)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        m.join({__shfl_xor_sync(0xffffffffu, m.sq, o), __shfl_xor_sync(0xffffffffu, m.sq_down, o), __shfl_xor_sync(0xffffffffu, m.top, o)});
+    for (int o = 16; o > 0; o >>= 1) m.join({__shfl_xor_sync(0xffffffffu, m.sq, o), __shfl_xor_sync(0xffffffffu, m.top, o)});
     if (TPR > 32) {
         if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
         __syncthreads();
@@ -196,17 +217,35 @@ __device__ __forceinline__ void row_reduce(RowSums &m, RowSums *sh)
         for (int w = 1; w < TPR / 32; ++w) m.join(sh[w]);
     }
 }
+template <int TPR>
+__device__ __forceinline__ float far_reduce(float f, RowSums *sh)
+{
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
+    if (TPR > 32) {
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5].sq = f;
+        __syncthreads();
+        f = 0.0f;
+#pragma unroll 1
+        for (int w = 0; w < TPR / 32; ++w) f += sh[w].sq;
+    }
+    return f;
+}
 
-// The row's scale (stored by `stores`), and what v is multiplied by before it is rounded.
-__device__ __forceinline__ float finish_row(const RmsArgs &a, const RowSums &m, long long row, bool stores)
+// The row's scale (stored by `stores`), and what v is multiplied by before it is rounded.  far: of the whole row, where it decides.
+__device__ __forceinline__ float finish_row(const RmsArgs &a, const RowSums &m, float far, long long row, bool stores)
 {
     const bool broken = !(m.top <= FLT_MAX);                       // a NaN or an infinity in the row
     const bool empty = m.top < TINY_ROW;
     float scale = m.top * (1.0f / 127.0f);
-    if (a.norm) {
-        // (where the squares of finite values do not fit, eps is nothing beside them)
-        if (m.sq <= FLT_MAX) scale *= 1.0f / sqrtf(fmaf(m.sq, a.inv_width, a.eps));
-        else scale = scale * DOWN / sqrtf(m.sq_down * a.inv_width);
+    if (!far_decides(a, m)) {
+        if (a.norm) scale *= 1.0f / sqrtf(fmaf(m.sq, a.inv_width, a.eps));
+    } else if (m.sq < LITTLE) {
+        const float root = sqrtf(fmaf(far, a.inv_width, a.eps * UP * UP));
+        scale = scale < 1.0f ? scale * UP / root : scale / root * UP;
+    } else {
+        scale /= fminf(sqrtf(far * a.inv_width) * (1.0f / DOWN), FLT_MAX);     // (eps is nothing here; the root itself is a float)
     }
     if (stores) a.scales[row] = broken ? __int_as_float(0x7fffffff) : empty ? 0.0f : scale;
     return broken || empty ? 0.0f : __fdiv_rn(127.0f, m.top);
@@ -230,7 +269,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
     T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
     int8_t *q = a.q + row * a.ldq;
     const int vecs = a.width / VE;
-    RowSums m = {0.0f, 0.0f, 0.0f};
+    RowSums m = {0.0f, 0.0f};
+    float far = 0.0f;
 
     // s of a vector, from what was loaded of x and the residual
     auto add = [&](const Raw<T, VE> &xr, const Raw<T, VE> &rr, float (&s)[VE]) {
@@ -262,6 +302,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
         if (a.g && !a.g_f32) gr = load_raw<T, VE>((const T *)a.g + at);
     };
 
+    // float rows, and rows that are not held, are read again in the rare case that the far sum decides; others keep it from the start
+    constexpr bool AGAIN = R == 0 || sizeof(T) == 4;
     float v[HELD][VE];
     if (R > 0) {
         Raw<T, VE> xr[HELD], rr[HELD], gr[HELD];
@@ -273,9 +315,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             if (at < vecs) {
                 add(xr[i], rr[i], v[i]);
                 if (out) store_elems<T, VE>(out + at * VE, v[i]);
-                if constexpr (VE == 1) {            // (both sums as they come cost a thread of single elements less than a second loop)
+                if constexpr (VE == 1 && AGAIN) {   // (single elements: one loop costs less than two)
                     m.sq = fmaf(v[i][0], v[i][0], m.sq);
-                    m.sq_down = fmaf(v[i][0] * DOWN, v[i][0] * DOWN, m.sq_down);
                     weigh(at, gr[i], v[i]);
                     m.largest(v[i]);
                 }
@@ -284,8 +325,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
                 for (int j = 0; j < VE; ++j) v[i][j] = 0.0f;
             }
         }
-        if constexpr (VE > 1) {
-            if (a.norm) m.squares(v);
+        if constexpr (VE > 1 || !AGAIN) {
+            if (a.norm) m.sq = AGAIN ? squares(v) : squares_and_far(v, a.eps, far);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const int at = i * TPR + t;
@@ -300,14 +341,27 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
             Raw<T, VE> xr, rr, gr;
             fetch(at, xr, rr, gr);
             add(xr, rr, v[0]);
-            m.squares(v);
+            m.sq += squares(v);
             weigh(at, gr, v[0]);
             m.largest(v[0]);
         }
     }
     row_reduce<TPR>(m, sh);
 
-    const float inv = finish_row(a, m, row, t == 0);
+    if (far_decides(a, m)) {
+        if constexpr (AGAIN)
+#pragma unroll 1
+            for (int at = t; at < vecs; at += TPR) {
+                Raw<T, VE> xr, rr, gr;
+                float s[1][VE];
+                fetch(at, xr, rr, gr);
+                if (R > 0 && out) to_float<T, VE>(load_raw<T, VE>(out + at * VE), s[0]);       // (it may be where x or the residual was; float: as it is)
+                else add(xr, rr, s[0]);
+                add_far(s, !(m.sq < LITTLE), far);
+            }
+        far = far_reduce<TPR>(far_part(m, far), sh);
+    }
+    const float inv = finish_row(a, m, far, row, t == 0);
 
     if (R > 0) {
 #pragma unroll
@@ -441,7 +495,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_shift_kernel(const 
     T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
     int8_t *q = a.q + row * a.ldq;
     const bool g_pairs = a.g && !a.g_f32;
-    RowSums m = {0.0f, 0.0f, 0.0f};
+    RowSums m = {0.0f, 0.0f};
+    float far = 0.0f;
     float v[R][VE];
     Pair xp[R], rp[R], gp[R];
 #pragma unroll
@@ -463,7 +518,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_shift_kernel(const 
         }
         if (out) store_shifted<T, VE>(out + at, v[i], count, lane);
     }
-    if (a.norm) m.squares(v);
+    if (a.norm) m.sq = squares_and_far(v, a.eps, far);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int at = (i * TPR + t) * VE, left = a.width - at, count = left < 0 ? 0 : left < VE ? left : VE;
@@ -479,7 +534,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_shift_kernel(const 
         m.largest(v[i]);
     }
     row_reduce<TPR>(m, sh);
-    const float inv = finish_row(a, m, row, t == 0);
+    if (far_decides(a, m)) far = far_reduce<TPR>(far_part(m, far), sh);
+    const float inv = finish_row(a, m, far, row, t == 0);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int at = (i * TPR + t) * VE, count = a.width - at;
@@ -607,7 +663,8 @@ __global__ void __launch_bounds__(32 * (STREAM_WARPS + STREAM_LOADERS), 1) rms_s
             if (!mbar_wait(smem_u32(&sh->full[stage]), parity, &sh->abort_flag)) gave_up(2);
             const uint32_t at = smem_u32(ring + (size_t)stage * s.stage_bytes) + (uint32_t)(t * 16);
             T *out = a.sum ? (T *)a.sum + row * a.lds : nullptr;
-            RowSums m = {0.0f, 0.0f, 0.0f};
+            RowSums m = {0.0f, 0.0f};
+            float far = 0.0f;
             float v[R][VE];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
@@ -630,7 +687,7 @@ __global__ void __launch_bounds__(32 * (STREAM_WARPS + STREAM_LOADERS), 1) rms_s
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->empty[stage]));             // the row is in registers
-            if (a.norm) m.squares(v);
+            if (a.norm) m.sq = squares_and_far(v, a.eps, far);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 if (i * TPR + t < vecs) {
@@ -649,14 +706,22 @@ __global__ void __launch_bounds__(32 * (STREAM_WARPS + STREAM_LOADERS), 1) rms_s
                 }
             }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-                m.join({__shfl_xor_sync(0xffffffffu, m.sq, o), __shfl_xor_sync(0xffffffffu, m.sq_down, o), __shfl_xor_sync(0xffffffffu, m.top, o)});
+            for (int o = 16; o > 0; o >>= 1) m.join({__shfl_xor_sync(0xffffffffu, m.sq, o), __shfl_xor_sync(0xffffffffu, m.top, o)});
             if (lane == 0) sh->sums[turn][warp - STREAM_LOADERS] = m;
             asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(TPR) : "memory");
             m = sh->sums[turn][group * GW];
 #pragma unroll
             for (int w = 1; w < GW; ++w) m.join(sh->sums[turn][group * GW + w]);
-            const float inv = finish_row(a, m, row, t == 0);
+            if (far_decides(a, m)) {
+                far = far_part(m, far);
+                for (int o = 16; o > 0; o >>= 1) far += __shfl_xor_sync(0xffffffffu, far, o);
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(TPR) : "memory");
+                if (lane == 0) sh->sums[turn][warp - STREAM_LOADERS].sq = far;
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(TPR) : "memory");
+                far = 0.0f;
+                for (int w = 0; w < GW; ++w) far += sh->sums[turn][group * GW + w].sq;
+            }
+            const float inv = finish_row(a, m, far, row, t == 0);
             int8_t *q = a.q + row * a.ldq;
 #pragma unroll
             for (int i = 0; i < R; ++i)
@@ -811,6 +876,7 @@ extern "C" int irms_quant(const irms_desc *desc, const void *x, const void *resi
         set_error("irms_quant: a row stride is shorter than the row");
         return ICONV_ERR_SHAPE;
     }
+    if (d.width > (1 << 24)) { set_error("irms_quant: width beyond 2^24"); return ICONV_ERR_SHAPE; }
     if (d.rows > 0x7fffffffll) { set_error("irms_quant: at most 2^31 - 1 rows"); return ICONV_ERR_SHAPE; }
     const long long most = 1ll << 46;                               // elements from a matrix's first row to its last
     if (d.rows > 0 && (d.x_stride > most / d.rows || d.q_stride > most / d.rows || (residual && d.residual_stride > most / d.rows) ||

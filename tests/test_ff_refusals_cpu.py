@@ -61,3 +61,17 @@ def test_tensors_are_read_by_plain_loads(file):
     text = open(os.path.join(CSRC, file)).read()
     assert "__restrict__" not in text and not re.search(r"\.nc\b", text) and "grid_dep_wait()" in text
     assert all(m.group(1).startswith("a.row_params") for m in re.finditer(r"__ldg\((.*)", text))
+
+
+def test_wider_rows_than_any():
+    """Indexes within a row are 32-bit numbers."""
+    for width in ((1 << 24) + 1, (1 << 31) - 1):
+        with pytest.raises(B.IconvError) as e:
+            _rms(rows=1, width=width)
+        assert e.value.status == B.ERR_SHAPE and "width" in B.iconv_last_error()
+
+
+def test_weights_further_apart_than_any():
+    with pytest.raises(B.IconvError) as e:
+        B.imat_plan(n=64, k=100, out_dtype=B.BF16, weights=A, scales=A, w_stride=1 << 60)
+    assert e.value.status == B.ERR_SHAPE

@@ -245,3 +245,21 @@ def test_no_rows_and_refusals_with_a_plan():
     for rows in (0, (1 << 30) + 1):
         with pytest.raises(B.IconvError):
             plan.describe(rows)
+
+
+def test_a_plan_is_refused_inside_a_capture_and_leaves_it_whole():
+    gen = generator(1)
+    f = Filter(gen, 64, 128)
+    x, sx = rows8(gen, 4, 128)
+    plan = Plan("f32", f)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph, out = torch.cuda.CUDAGraph(), torch.zeros(4, 64, device="cuda")
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        with pytest.raises(B.IconvError) as e:
+            Plan("f32", f)
+        assert e.value.status == B.ERR_CUDA and "capturing" in B.iconv_last_error()
+        plan(x, sx, out=out)
+    graph.replay()
+    torch.cuda.synchronize()
+    plan.check(x, sx, out)

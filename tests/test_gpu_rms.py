@@ -245,3 +245,64 @@ def test_bad_values_beside_a_row_do_not_reach_it(dtype):
     q, scales, total = rms_call(x, q=torch.empty(m, 528, dtype=torch.int8, device="cuda")[:, :d])
     assert torch.equal(q[::2], clean[0][::2]) and torch.equal(total[::2], clean[2][::2]) and torch.isnan(scales[1::2]).all()
     assert ((scales - clean[1]).abs()[::2] <= 40 * 2.0 ** -24 * scales[::2]).all()
+
+
+@pytest.mark.parametrize("d", [1 << 24, (1 << 24) - 3])
+def test_the_widest_row(d):
+    x, _, g = _data(d, 1, d, "bf16", residual=False)
+    rms_check(x, None, g, *rms_call(x, None, g))
+    with pytest.raises(B.IconvError):
+        B.irms_quant(ptr(x), None, None, None, ptr(x), ptr(x), stream(), rows=1, width=(1 << 24) + 1, dtype=B.BF16)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [40, 333, 700, 4104, 40000, 40001])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-12])
+def test_squares_too_small_to_hold(dtype, d, eps):
+    """Rows whose squares vanish in float, in part or all, beside an eps that does not cover them."""
+    size = torch.tensor([1e-34, 1e-30, 1e-25, 1e-21, 1e-18, 1e-14, 1e-10, 1e-8], device="cuda")[:, None]
+    x = (torch.randn(8, d, generator=generator(1), device="cuda") * size).to(TYPES[dtype])
+    x[4:6, ::3] *= 1e-7                                     # (large and small ones in a row)
+    for g in (None, (1e4 * torch.rand(d, generator=generator(2), device="cuda")).to(TYPES[dtype]), torch.full((d,), 1e30, device="cuda").to(TYPES[dtype])):
+        q, scales, total = rms_call(x, None, g, eps=eps)
+        rms_check(x, None, g, q, scales, total, eps=float(torch.tensor(eps)))      # (eps is a float)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 333, 700, 40000])
+def test_large_rows_times_small_weights(dtype, d):
+    x = (torch.randn(3, d, generator=generator(1), device="cuda") * torch.tensor([1e19, 1e25, 1e37], device="cuda")[:, None]).to(TYPES[dtype])
+    g = torch.full((d,), 2e-31, device="cuda").to(TYPES[dtype])
+    q, scales, total = rms_call(x, None, g)
+    rms_check(x, None, g, q, scales, total)
+
+
+def test_many_small_wide_rows():
+    m, d = 148 * 4 + 3, 8192
+    x = (torch.randn(m, d, generator=generator(1), device="cuda") * 10.0 ** -torch.randint(10, 35, (m, 1), generator=generator(2), device="cuda")).bfloat16()
+    rms_check(x, None, None, *rms_call(x, eps=0.0), eps=0.0)
+
+
+FIRST = """
+import torch
+from paper_2006_11735_b200 import binding as B
+x = torch.randn(%(m)d, %(d)d, device="cuda").bfloat16()
+q, scales = torch.empty(%(m)d, %(d)d, dtype=torch.int8, device="cuda"), torch.empty(%(m)d, device="cuda")
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    B.irms_quant(x.data_ptr(), None, None, None, q.data_ptr(), scales.data_ptr(), torch.cuda.current_stream().cuda_stream, rows=%(m)d, width=%(d)d, dtype=B.BF16)
+graph.replay()
+torch.cuda.synchronize()
+got = q.float() * scales[:, None]
+want = x.float() * (x.float().pow(2).mean(1, keepdim=True) + 1e-5).rsqrt()
+assert ((got - want).abs() <= 0.51 * scales[:, None]).all()
+print("captured first")
+"""
+
+
+@pytest.mark.parametrize("m,d", [(3, 64), (3, 333), (700, 8192)])
+def test_the_first_call_of_a_process_is_captured(m, d):
+    import subprocess
+    import sys
+    done = subprocess.run([sys.executable, "-c", FIRST % dict(m=m, d=d)], capture_output=True, text=True, timeout=120, cwd=B.__file__.rsplit("/", 2)[0])
+    assert done.returncode == 0 and "captured first" in done.stdout, done.stderr[-2000:]
