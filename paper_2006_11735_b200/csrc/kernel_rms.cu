@@ -382,10 +382,11 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
 }
 
 // ---- Rows of 16-bit elements that start anywhere (an odd width without padding): vectors of 16 bytes all the same (2000 rows of 16001 with a
-// residual: 92 us, 367 element by element; 8192 of 4001 alone 44 and 80; in float single elements are as fast: 82 us, 124 so).  A thread's VE elements lie across two aligned 16-byte
-// words; both are loaded (the second is the neighbour's first, and in L1) and shifted by the row's phase, which is the same for all its threads.
-// The sum goes back the other way: a lane stores the aligned word that its own elements and the lane's before it make up, and the ends of a
-// warp's stretch go out element by element.  q's rows are aligned.
+// residual: 86 us, 367 element by element; 8192 of 4001 alone 46 and 80; in float single elements are as fast: 4000 of 1501 18 us, 20 so, 2000 of 8191 54 and 54).  A thread's VE
+// elements lie across two aligned 16-byte words; both are loaded (the second is the neighbour's first, and in L1) and shifted by the row's phase,
+// which is the same for all its threads.  The sum goes back the other way: a lane stores the aligned word that its own elements and the
+// lane's before it make up, and the ends of a warp's stretch go out element by element.  q's rows are aligned.
+// 1024 threads of 64 registers on an SM, at the price of a word or two of spills (82 registers: 2000 rows of 8191 with a residual 58 us, 40 so).
 
 // Bytes off ... off + 15 of the 32 that a and b make.
 __device__ __forceinline__ uint4 cut16(const uint4 &a, const uint4 &b, unsigned off)
@@ -481,7 +482,7 @@ struct ShiftArgs {
 };
 
 template <typename T, int TPR, int R>
-__global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_shift_kernel(const __grid_constant__ ShiftArgs s)
+__global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 1024 ? 1 : TPR >= 256 ? 1024 / TPR : 8) rms_shift_kernel(const __grid_constant__ ShiftArgs s)
 {
     constexpr int VE = 16 / (int)sizeof(T), ROWS = TPR > 128 ? 1 : 128 / TPR;
     __shared__ RowSums sh[ROW_WARPS_MAX];
@@ -584,7 +585,7 @@ cudaError_t launch_shift(const ShiftArgs &s, cudaStream_t stream)
     if (vecs <= 256) return launch_shift_one<T, 128, 2>(s, stream);
     if (vecs <= 512) return launch_shift_one<T, 256, 2>(s, stream);
     if (vecs <= 1024) return launch_shift_one<T, 512, 2>(s, stream);
-    return launch_shift_one<T, 512, 4>(s, stream);
+    return launch_shift_one<T, 1024, 2>(s, stream);
 }
 
 // Many wide rows: one block per SM, whose loading warps keep a ring of whole rows in shared memory ahead of the arithmetic, so that the memory
@@ -761,9 +762,15 @@ cudaError_t launch_width(const RmsArgs &a, cudaStream_t stream)
         if (vecs <= 4096) return launch_one<T, VE, 1024, 4>(a, stream);
         return launch_one<T, VE, 1024, 0>(a, stream);
     } else {
+        // (instances within a factor of two of the width: what a thread asks for beyond the row's end costs as much as the rest -- 20000
+        // float rows of 255 take 13 us with eight elements a lane, 33 with eight in each thread of four warps; 2000 of 5001 47 and, over 1024 threads, 81)
         if (vecs <= 128) return launch_one<T, VE, 32, 4>(a, stream);
+        if (vecs <= 256) return launch_one<T, VE, 32, 8>(a, stream);
+        if (vecs <= 512) return launch_one<T, VE, 128, 4>(a, stream);
         if (vecs <= 1024) return launch_one<T, VE, 128, 8>(a, stream);
+        if (vecs <= 2048) return launch_one<T, VE, 256, 8>(a, stream);
         if (vecs <= 4096) return launch_one<T, VE, 256, 16>(a, stream);
+        if (vecs <= 8192) return launch_one<T, VE, 512, 16>(a, stream);
         if (vecs <= 16384) return launch_one<T, VE, 1024, 16>(a, stream);
         return launch_one<T, VE, 1024, 0>(a, stream);
     }
