@@ -385,9 +385,9 @@ def iconv_stem_forward_static(x_ptr, weights_ptr, bias_ptr, out_ptr, stream=0, *
 def irms_quant(x_ptr, residual_ptr, weight_ptr, sum_ptr, q_ptr, scales_ptr, stream=0, *, rows, width, dtype, weight_dtype=None, eps=0.0, norm=1,
                x_stride=None, residual_stride=None, sum_stride=None, q_stride=None):
     """Residual addition, root-mean-square norm and 8-bit rows with a scale each; strides in elements (default: dense rows)."""
-    dense = lambda s: width if s is None else s
-    d = irms_desc(rows=rows, width=width, dtype=dtype, weight_dtype=dtype if weight_dtype is None else weight_dtype, norm=norm, eps=eps,
-                  x_stride=dense(x_stride), residual_stride=dense(residual_stride), sum_stride=dense(sum_stride), q_stride=dense(q_stride))
+    # (fields by position, in the struct's order: by name they cost a call 0.4 us more)
+    d = irms_desc(rows, width, dtype, dtype if weight_dtype is None else weight_dtype, norm, eps, width if x_stride is None else x_stride,
+                  width if residual_stride is None else residual_stride, width if sum_stride is None else sum_stride, width if q_stride is None else q_stride)
     _check(lib.irms_quant(C.byref(d), x_ptr, residual_ptr, weight_ptr, sum_ptr, q_ptr, scales_ptr, stream))
 
 

@@ -15,7 +15,7 @@ struct imat_plan_s {
     int n = 0, k = 0, out_dtype = 0, act = 0, gated = 0, device = -1, sms = 0;
     int ch_tiles = 0, k_blocks = 0;
     int8_t *packed = nullptr;              // [ch_tiles][k_blocks][128 rows][128 bytes]
-    float2 *row_params = nullptr;          // [ch_tiles * 128] scale, bias
+    float2 *row_params = nullptr;          // behind them: [ch_tiles * 128] scale, bias
     CUtensorMap tmap_w;
 };
 
@@ -236,8 +236,8 @@ int build_plan(const imat_desc &d, cudaStream_t stream, imat_plan_t *p)
     if (rc != ICONV_OK) return rc;
     p->device = current_device_slot();
     const size_t bytes = (size_t)p->ch_tiles * p->k_blocks * MAT_BLOCK;
-    ICONV_CUDA_TRY(cudaMalloc((void **)&p->packed, bytes));
-    ICONV_CUDA_TRY(cudaMalloc((void **)&p->row_params, (size_t)p->ch_tiles * BLOCK_M * sizeof(float2)));
+    ICONV_CUDA_TRY(cudaMalloc((void **)&p->packed, bytes + (size_t)p->ch_tiles * BLOCK_M * sizeof(float2)));
+    p->row_params = (float2 *)(p->packed + bytes);
     rc = umma_encode_2d(&p->tmap_w, p->packed, 128, (long long)(bytes / 128), 128, 128, BLOCK_M, 128);
     if (rc != ICONV_OK) return rc;
     PackArgs a;
@@ -265,7 +265,6 @@ extern "C" int imat_plan_destroy(imat_plan_t *p)
 {
     if (!p) return ICONV_OK;
     cudaFree(p->packed);
-    cudaFree(p->row_params);
     delete p;
     return ICONV_OK;
 }
