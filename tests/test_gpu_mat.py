@@ -263,3 +263,28 @@ def test_a_plan_is_refused_inside_a_capture_and_leaves_it_whole():
     graph.replay()
     torch.cuda.synchronize()
     plan.check(x, sx, out)
+
+
+@pytest.mark.parametrize("m,step,n,gated,k", [(40, 1 << 27, 4000, False, 144), (40, 1 << 27, 300, True, 144), (2100, 1 << 22, 2600, False, 144), (2100, 1 << 22, 2600, True, 144),
+                                              (2100, 1 << 22, 5000, False, 1000), (2100, 1 << 22, 5000, True, 1000)])
+def test_far_rows_on_the_other_kernels(m, step, n, gated, k):
+    """x and out more than 4 GB from their first row to their last, the residual more than 2^31 elements."""
+    gen = generator(19)
+    plan = Plan("bf16", Filter(gen, n, k), Filter(gen, n, k) if gated else None)
+    assert k == 144 or plan.describe(m).startswith("bulk")
+    x = torch.empty(m * step, dtype=torch.int8, device="cuda").view(m, step)[:, :k]
+    x.copy_(rows8(gen, m, k)[0])
+    sx = torch.rand(m, generator=gen, device="cuda")
+    out = torch.empty(m * step, dtype=torch.bfloat16, device="cuda").view(m, step)[:, 1:n + 1]
+    r = None
+    if not gated:
+        r = torch.empty(m * step, dtype=torch.bfloat16, device="cuda").view(m, step)[:, :n]
+        r.copy_(torch.randn(m, n, generator=gen, device="cuda"))
+    plan(x, sx, r, out)
+    plan.check(x, sx, out.contiguous(), r)
+
+
+def test_very_many_rows():
+    plan, x, sx, _ = _case(20, (1 << 24) + 3, 16, 3, "f32")
+    plan.check(x, sx, plan(x, sx))
+    B.iconv_check(stream())

@@ -306,3 +306,19 @@ def test_the_first_call_of_a_process_is_captured(m, d):
     import sys
     done = subprocess.run([sys.executable, "-c", FIRST % dict(m=m, d=d)], capture_output=True, text=True, timeout=120, cwd=B.__file__.rsplit("/", 2)[0])
     assert done.returncode == 0 and "captured first" in done.stdout, done.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m,d,step", [(5, 4000, (1 << 30) + 1), (5, 20001, (1 << 30) + 1), (700, 8192, 1 << 23)])
+def test_far_rows_of_every_kind(m, d, step):
+    """Cut out of words, single elements, streams: more than 4 GB from the first row to the last, in q too."""
+    gen = generator(d)
+    x = torch.empty(m * step, dtype=torch.bfloat16, device="cuda").view(m, step)[:, :d]
+    x.copy_(torch.randn(m, d, generator=gen, device="cuda"))
+    q = torch.empty(m * step, dtype=torch.int8, device="cuda").view(m, step)[:, :d]
+    q, scales, total = rms_call(x, q=q, total=x)
+    rms_check(x, None, None, q, scales, total)
+
+
+def test_very_many_rows():
+    x, r, g = _data(5, (1 << 25) + 1, 3, "bf16")
+    rms_check(x, r, g, *rms_call(x, r, g))
