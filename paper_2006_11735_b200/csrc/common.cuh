@@ -35,6 +35,8 @@ struct ConvArgs {
 // stream has completed and its writes are visible: every role executes it before it first touches
 // a tensor another kernel may have written (activations, skip); plan-owned constants may be read
 // before.  grid_dep_launch tells the scheduler that the kernel after this one may be scheduled.
+// A kernel with tensor memory executes it once the block has that memory (in every kernel with a tcgen05.alloc: behind the barrier that
+// follows it): a block of the next kernel that got it first would hold it while it waits for this kernel, which then never ends.
 // Tensors are read by plain loads in such a kernel, never by __ldg or through a const __restrict__ pointer: the read-only path is for
 // what nothing writes while the kernel runs, and here the kernel before it may.
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -183,7 +183,6 @@ picture_kernel(const __grid_constant__ PicArgs u, const __grid_constant__ ConvAr
         mbar_init(smem_u32(&sh->drain), PIC_GROUPS);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        grid_dep_launch();
     }
     // operand rows of 32 bytes, 32-byte swizzle: the halves of rows 4 to 7 of every eight change places
     if ((int)threadIdx.x < 2 * bn) {
@@ -195,6 +194,7 @@ picture_kernel(const __grid_constant__ PicArgs u, const __grid_constant__ ConvAr
     if (warp == 0) tmem_alloc(smem_u32(&sh->tmem_base), (uint32_t)u.tmem_cols);
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
     grid_dep_wait();               // the picture may come from, and the output may still be read by, the kernel before this one

@@ -278,7 +278,7 @@ __device__ __forceinline__ uint32_t mat_set_up(MatShared *sh, const MatArgs &a, 
     }
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0) grid_dep_launch();     // (not before this block has its tensor memory: a block of the next kernel could take it first and wait for this kernel's end)
+    if (threadIdx.x == 0) grid_dep_launch();     // (behind the tensor memory: see grid_dep_launch)
     if (PAIR) cluster_sync_all();                // the peer's barriers exist before anything arrives at them
     tc_fence_after();
     return sh->tmem_base;

@@ -110,11 +110,11 @@ umma_chain_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_const
         mbar_init(smem_u32(&sh->drain), 1);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        grid_dep_launch();
     }
     if (warp == MMA_WARP) tmem_alloc(smem_u32(&sh->tmem_base), 512u);
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
 

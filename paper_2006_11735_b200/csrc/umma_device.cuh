@@ -803,7 +803,6 @@ umma_conv_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         mbar_init(smem_u32(&sh->drain), 1);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        grid_dep_launch();
     }
     if (warp == MMA_WARP) {
         if (PAIR) tmem_alloc_pair(smem_u32(&sh->tmem_base), (uint32_t)u.tmem_cols);
@@ -811,6 +810,7 @@ umma_conv_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
     }
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();
     if (PAIR) cluster_sync_all();            // the peer's barriers exist before anything arrives at them
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
@@ -1378,11 +1378,11 @@ umma_window_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_cons
         mbar_init(smem_u32(&sh->drain), WIN_ISSUERS);          // one arrival per MMA issuer
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        grid_dep_launch();
     }
     if (warp == MMA_WARP) tmem_alloc(smem_u32(&sh->tmem_base), (uint32_t)u.tmem_cols);
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
 

@@ -122,7 +122,6 @@ umma_roll_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         sh->go = 0;
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        grid_dep_launch();
     }
     if (threadIdx.x == 32) {
         prefetch_tensormap(&map_x);
@@ -131,6 +130,7 @@ umma_roll_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     if (warp == MMA_WARP) tmem_alloc(smem_u32(&sh->tmem_base), (uint32_t)u.tmem_cols);
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0) grid_dep_launch();
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
 

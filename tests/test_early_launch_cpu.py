@@ -64,3 +64,18 @@ def test_a_kernel_that_comes_up_early_reads_its_tensors_by_plain_loads(name):
 def test_the_tensor_core_kernels_read_their_tensors_by_plain_loads(file):
     assert "__restrict__" not in SOURCES[file]
     _constants_only(SOURCES[file], file)
+
+
+def test_the_next_kernel_comes_up_behind_the_tensor_memory():
+    """A block that signals before it has its tensor memory may lose it to a block of the next kernel, which waits for this kernel's end:
+    neither would ever go on."""
+    found = []
+    for file, text in SOURCES.items():
+        for body in text.split("\n}\n"):
+            takes = [m.start() for m in re.finditer(r"\btmem_alloc(?:_pair)?\(smem_u32", body)]
+            lets = [m.start() for m in re.finditer(r"\bgrid_dep_launch\(\);", body)]
+            if takes and lets:
+                found.append(file)
+                assert max(takes) < min(lets) and "__syncthreads();" in body[max(takes):min(lets)], file
+    assert sorted(found) == ["kernel_picture.cu", "kernel_pool.cu", "mat_device.cuh", "umma_chain.cuh", "umma_device.cuh", "umma_device.cuh", "umma_flow.cuh",
+                             "umma_roll.cuh", "umma_stack.cuh"]
