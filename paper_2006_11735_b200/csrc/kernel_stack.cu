@@ -154,7 +154,10 @@ int stack_geometry(iconv_stack_t *s)
     u.desc_hi_a = p->win_blocks ? (unsigned)((((unsigned long long)((p->win_bw * p->kc) >> 4) << 32) | (1ull << 46) | (layout << 61)) >> 32) : u.desc_hi_b;
     umma_find_divisor((unsigned)u.tpi, u.div_tpi_mul, u.div_tpi_shr);
     umma_find_divisor((unsigned)u.vw, u.div_vw_mul, u.div_vw_shr);
-    s->smem = (size_t)fixed + (size_t)u.stages * u.stage_bytes;
+    // All of it, needed (130 to 184 KB of it) or not: a CTA has its SM to itself.  Its tensor memory is all there is, and with room left on the SM a
+    // block of a cluster in another stream could hold some of it and wait for its peer, which waits on another SM for what a CTA
+    // of this launch holds there, which waits for this one.  (Twenty layers of 16 x 256 x 256 take as long either way.)
+    s->smem = MAX_SMEM;
     // what the shared epilogue reads of the single-layer kernels' arguments
     memset(&s->a, 0, sizeof(s->a));
     memset(&s->ua, 0, sizeof(s->ua));

@@ -311,3 +311,34 @@ def test_run_of_layers_refuses_what_it_cannot_take():
         with pytest.raises(B.IconvError) as e:
             B.iconv_plan_stack(bad)
         assert e.value.status == B.ERR_UNSUPPORTED
+
+
+def test_beside_products_whose_blocks_share_a_reduction():
+    """A stack's CTAs wait on one another, and so do the blocks of a cluster of ``imat_forward``: on two streams at once each finds its
+    tensor memory on every SM, or none.  (Stacks of 48 channels leave 96 KB of an SM's shared memory, the first product's blocks take 81 KB.)"""
+    from ff_util import Filter, Plan, generator, rows8
+    net = N.vdsr(n=1, h=97, w=321, width=48)
+    g = Network(net, load_params("vdsr"))
+    assert g.stacks
+    x = torch.from_numpy(gen.uniform_u8(3, (1, 97, 321, 1))).cuda()
+    want = g.forward(x).clone()
+    products = []
+    for m, n, k in ((506, 1, 1872), (24, 300, 4096)):
+        plan = Plan("f32", Filter(generator(k), n, k), act="silu")
+        assert plan.describe(m).startswith("few") and "split 1," not in plan.describe(m)
+        r = torch.randn(m, n, generator=generator(m), device="cuda")
+        q, scale = rows8(generator(k), m, k)
+        products.append((plan, q, scale, r, plan(q, scale, r)))
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    different = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(100):
+        with torch.cuda.stream(other):
+            got = [(plan(q, scale, r), right) for plan, q, scale, r, right in products for _ in range(5)]
+        different += (g.forward(x) != want).sum()
+        torch.cuda.current_stream().wait_stream(other)
+        for out, right in got:
+            different += (out != right).sum()
+    _check()
+    assert int(different) == 0 and int(g.sync.sum()) == 0
+    g.close()

@@ -61,3 +61,11 @@ def test_an_empty_batch_without_tensors_is_left_to_single_launches(k):
     with pytest.raises(B.IconvError) as e:
         B.iconv_plan_stack([(_layer(k), 0, C), (_layer(k), C, D)])
     assert e.value.status == B.ERR_ARG
+
+
+def test_a_stack_has_its_sms_to_itself():
+    """... by asking for all of the shared memory, whatever the layers need of it."""
+    import os
+    from paper_2006_11735_b200.build import CSRC
+    text = open(os.path.join(CSRC, "kernel_stack.cu")).read()
+    assert "s->smem = MAX_SMEM;" in text and "cfg.dynamicSmemBytes = s->smem;" in text
