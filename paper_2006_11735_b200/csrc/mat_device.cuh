@@ -82,18 +82,48 @@ template <> __device__ __forceinline__ __nv_bfloat16 mat_round<__nv_bfloat16>(fl
 // y / (1 + exp(-z)): both smooth activations but one are of this form
 __device__ __forceinline__ float mat_sigmoid_times(float y, float z) { return __fdividef(y, 1.0f + __expf(-z)); }
 
-// y / 2 * (1 + erf(y / sqrt 2)) = y / 2 * (2 - e) or y / 2 * e, e = erfc(|y| / sqrt 2), by the rational approximation 7.1.26 of Abramowitz and
-// Stegun, Handbook of Mathematical Functions: e = (a1 t + ... + a5 t^5) exp(-y^2 / 2), t = 1 / (1 + p |y| / sqrt 2), off by 1.5e-7 at most, a third of the
-// instructions of an error function for every argument.
-__device__ __forceinline__ float mat_gelu(float y)
+// 2^x and 1 / x to two steps, x normal; results that are no normal numbers are zero
+__device__ __forceinline__ float mat_exp2(float x)
 {
-    const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(y), 1.0f));
-    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float e = poly * __expf(-0.5f * y * y);
-    return 0.5f * y * (y < 0.0f ? e : 2.0f - e);
+    float d;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+    return d;
+}
+__device__ __forceinline__ float mat_reciprocal(float x)
+{
+    float d;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+    return d;
 }
 
-template <int N>
+// y / 2 * (1 + erf(y / sqrt 2)) = y / 2 * erfc(-y / sqrt 2), where the factor is e = erfc(|y| / sqrt 2) = exp(-y^2 / 2) (c1 t + c2 t^2 + ...), t = 1 / (1 + c |y|), for
+// y < 0 and 2 - e for the others: nothing cancels on the negative side, where the value falls to nothing.  The polynomials are fits for these kernels: least
+// squares over |y| of 0 ... 15, weighted anew until the error is even (Lawson's iteration).  FINE (float results): of the relative error, 7e-9 in exact arithmetic and 4e-7 at
+// most in float.  16-bit results: of the error in units of 3e-7 for e and 5e-6 relative, the larger; 4e-7 for e and 1.9e-6 relative in float.  (CUDA's erfc for float results
+// took 4096 x 1024 x 4096 from 33 us to 55.)
+template <bool FINE>
+__device__ __forceinline__ float mat_gelu(float y)
+{
+    const float half = __fmul_rn(0.5f, y);
+    const float t = mat_reciprocal(fmaf(FINE ? 0.246f : 0.26f, fabsf(y), 1.0f));
+    float p, e;
+    if (FINE) {
+        p = fmaf(t, 0.0419157145f, -0.181555882f);
+        p = fmaf(t, p, 0.236114511f); p = fmaf(t, p, -0.0902956311f); p = fmaf(t, p, 0.134590968f); p = fmaf(t, p, 0.123590758f);
+        p = fmaf(t, p, 0.157703434f); p = fmaf(t, p, 0.185537543f); p = fmaf(t, p, 0.196109322f); p = fmaf(t, p, 0.196289268f);
+        e = expf(__fmul_rn(-half, y));
+    } else {
+        p = fmaf(t, -0.145882931f, 0.45747601f);
+        p = fmaf(t, p, -0.211728841f); p = fmaf(t, p, 0.331641501f); p = fmaf(t, p, 0.147230836f); p = fmaf(t, p, 0.214217862f);
+        p = fmaf(t, p, 0.207045531f);
+        const float z = __fmul_rn(0.849321800f, y);        // z^2 = y^2 / 2 / log 2
+        e = mat_exp2(-__fmul_rn(z, z));
+    }
+    e = __fmul_rn(__fmul_rn(t, p), e);
+    return __fmul_rn(half, y < 0.0f ? e : __fadd_rn(2.0f, -e));
+}
+
+template <bool FINE, int N>
 __device__ __forceinline__ void mat_act(int act, float (&y)[N])
 {
     switch (act) {
@@ -107,7 +137,7 @@ __device__ __forceinline__ void mat_act(int act, float (&y)[N])
         break;
     case IMAT_GELU:
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = mat_gelu(y[j]);
+        for (int j = 0; j < N; ++j) y[j] = mat_gelu<FINE>(y[j]);
         break;
     case IMAT_GELU_TANH:            // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
 #pragma unroll
@@ -160,7 +190,7 @@ __device__ __forceinline__ void mat_values(const MatArgs &a, const int (&acc)[P]
 #pragma unroll
     for (int j = 0; j < P; ++j) y[j] = fmaf((float)acc[j] * par.x, sx[j], par.y);
     if (!GATED) {
-        mat_act<P>(a.act, y);
+        mat_act<sizeof(T) == 4, P>(a.act, y);
         if (a.residual)
 #pragma unroll
             for (int j = 0; j < P; ++j) y[j] += mat_value<T>(res[j]);
@@ -174,7 +204,7 @@ __device__ __forceinline__ void mat_values(const MatArgs &a, const int (&acc)[P]
             g[p] = up_lane ? other : y[2 * p];
             u[p] = up_lane ? y[2 * p + 1] : other;
         }
-        mat_act<P / 2>(a.act, g);
+        mat_act<sizeof(T) == 4, P / 2>(a.act, g);
 #pragma unroll
         for (int p = 0; p < P / 2; ++p) y[p] = g[p] * u[p];
     }

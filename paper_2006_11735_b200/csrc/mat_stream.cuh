@@ -125,10 +125,10 @@ mat_stream_kernel(const __grid_constant__ MatStreamArgs s, const __grid_constant
         float y[1] = {fmaf((float)total * par.x, sx, par.y)};
         if (GATED) {
             const float up = __shfl_xor_sync(0xffffffffu, y[0], 16);
-            mat_act<1>(a.act, y);
+            mat_act<sizeof(T) == 4, 1>(a.act, y);
             y[0] *= up;
         } else {
-            mat_act<1>(a.act, y);
+            mat_act<sizeof(T) == 4, 1>(a.act, y);
             if (a.residual) y[0] += res;
         }
         if (stores) ((T *)a.out)[tok * a.ld_out + ch] = mat_round<T>(y[0]);
