@@ -79,9 +79,6 @@ template <> __device__ __forceinline__ float mat_round<float>(float v) { return 
 template <> __device__ __forceinline__ __half mat_round<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 mat_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// y / (1 + exp(-z)): both smooth activations but one are of this form
-__device__ __forceinline__ float mat_sigmoid_times(float y, float z) { return __fdividef(y, 1.0f + __expf(-z)); }
-
 // 2^x and 1 / x to two steps, x normal; results that are no normal numbers are zero
 __device__ __forceinline__ float mat_exp2(float x)
 {
@@ -94,6 +91,18 @@ __device__ __forceinline__ float mat_reciprocal(float x)
     float d;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
     return d;
+}
+
+// y / (1 + exp(-z)) of SiLU and tanh-GELU, as y e / (1 + e) for z < 0, e = exp(-|z|): neither the exponential nor the quotient leaves float's range.  FINE
+// (float results): z as it is, expf, a reciprocal with a Newton step.  16-bit results: z / log 2; values under |y| 2^-126 are zero.
+template <bool FINE>
+__device__ __forceinline__ float mat_sigmoid_times(float y, float z)
+{
+    const float e = FINE ? expf(-fabsf(z)) : mat_exp2(-fabsf(z));
+    const float d = __fadd_rn(1.0f, e);
+    float r = mat_reciprocal(d);
+    if (FINE) r = fmaf(r, fmaf(-d, r, 1.0f), r);
+    return __fmul_rn(z < 0.0f ? __fmul_rn(y, e) : y, r);
 }
 
 // y / 2 * (1 + erf(y / sqrt 2)) = y / 2 * erfc(-y / sqrt 2), where the factor is e = erfc(|y| / sqrt 2) = exp(-y^2 / 2) (c1 t + c2 t^2 + ...), t = 1 / (1 + c |y|), for
@@ -133,7 +142,7 @@ __device__ __forceinline__ void mat_act(int act, float (&y)[N])
         break;
     case IMAT_SILU:
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = mat_sigmoid_times(y[j], y[j]);
+        for (int j = 0; j < N; ++j) y[j] = mat_sigmoid_times<FINE>(y[j], FINE ? y[j] : __fmul_rn(1.44269504f, y[j]));
         break;
     case IMAT_GELU:
 #pragma unroll
@@ -141,7 +150,8 @@ __device__ __forceinline__ void mat_act(int act, float (&y)[N])
         break;
     case IMAT_GELU_TANH:            // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = mat_sigmoid_times(y[j], y[j] * fmaf(0.0713548162726f, y[j] * y[j], 1.5957691216057f));
+        for (int j = 0; j < N; ++j)
+            y[j] = mat_sigmoid_times<FINE>(y[j], __fmul_rn(y[j], fmaf(FINE ? 0.0713548162726f : 0.102943240f, __fmul_rn(y[j], y[j]), FINE ? 1.5957691216057f : 2.302208198f)));
         break;
     default: break;
     }
