@@ -193,17 +193,19 @@ __device__ __forceinline__ void mat_load_residual(const MatArgs &a, long long to
         r += j < last ? a.ld_res : 0;
     }
 }
+// Every product and sum from here to the rounding is one operation of its own or an fmaf: the compiler may fuse others, and not the same ones in every kernel, but
+// a row is the same whichever kernel a call runs.
 // What the lane stores, from the sums: y[j] of token tok + j, or, gated, of token tok + 2 j + (lane >= 16) for j < P / 2.
 template <typename T, bool GATED, int P>
 __device__ __forceinline__ void mat_values(const MatArgs &a, const int (&acc)[P], const float (&sx)[P], const T (&res)[P], float2 par, int lane, float (&y)[P])
 {
 #pragma unroll
-    for (int j = 0; j < P; ++j) y[j] = fmaf((float)acc[j] * par.x, sx[j], par.y);
+    for (int j = 0; j < P; ++j) y[j] = fmaf(__fmul_rn((float)acc[j], par.x), sx[j], par.y);
     if (!GATED) {
         mat_act<sizeof(T) == 4, P>(a.act, y);
         if (a.residual)
 #pragma unroll
-            for (int j = 0; j < P; ++j) y[j] += mat_value<T>(res[j]);
+            for (int j = 0; j < P; ++j) y[j] = __fadd_rn(y[j], mat_value<T>(res[j]));
     } else {
         // lanes 0-15 hold the gate of 16 channels, lanes 16-31 their up projection: of two tokens the lower lanes finish the first, the upper ones the second
         const bool up_lane = lane >= 16;
@@ -216,7 +218,7 @@ __device__ __forceinline__ void mat_values(const MatArgs &a, const int (&acc)[P]
         }
         mat_act<sizeof(T) == 4, P / 2>(a.act, g);
 #pragma unroll
-        for (int p = 0; p < P / 2; ++p) y[p] = g[p] * u[p];
+        for (int p = 0; p < P / 2; ++p) y[p] = __fmul_rn(g[p], u[p]);
     }
 }
 // WHOLE: every token exists, and every lane's channel.

@@ -122,14 +122,14 @@ mat_stream_kernel(const __grid_constant__ MatStreamArgs s, const __grid_constant
         if (!GATED && a.residual && stores) res = mat_value<T>(((const T *)a.residual)[tok * a.ld_res + ch]);
         int total = 0;
         for (int i = 0; i < warps; ++i) total += sums[(i * (TOKENS8 * 8) + tok) * MAT_STREAM_PITCH + lane];
-        float y[1] = {fmaf((float)total * par.x, sx, par.y)};
+        float y[1] = {fmaf(__fmul_rn((float)total, par.x), sx, par.y)};
         if (GATED) {
             const float up = __shfl_xor_sync(0xffffffffu, y[0], 16);
             mat_act<sizeof(T) == 4, 1>(a.act, y);
-            y[0] *= up;
+            y[0] = __fmul_rn(y[0], up);
         } else {
             mat_act<sizeof(T) == 4, 1>(a.act, y);
-            if (a.residual) y[0] += res;
+            if (a.residual) y[0] = __fadd_rn(y[0], res);
         }
         if (stores) ((T *)a.out)[tok * a.ld_out + ch] = mat_round<T>(y[0]);
     }

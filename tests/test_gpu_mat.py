@@ -288,3 +288,25 @@ def test_very_many_rows():
     plan, x, sx, _ = _case(20, (1 << 24) + 3, 16, 3, "f32")
     plan.check(x, sx, plan(x, sx))
     B.iconv_check(stream())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("form", ["gated", "residual", "neither"])
+def test_a_row_is_the_same_in_any_call_whatever_the_activation(form, act, dtype):
+    """Products and sums behind one another, in kernels that are compiled apart."""
+    plan, x, sx, r = _case(21, 2500, 1030, 2500, dtype, act, form == "gated", residual=form == "residual")
+    whole = plan(x, sx, r)
+    assert plan.describe(2500).startswith("bulk")
+    forms = set()
+    for m, kernel in ((1, "stream"), (9, "stream"), (20, "few"), (64, "few"), (100, "few")):
+        assert plan.describe(m).startswith(kernel)
+        forms.add(kernel + (" alone" if "split 1," in plan.describe(m) else ""))
+        some = plan(x[1000:1000 + m], sx[1000:1000 + m].clone(), r[1000:1000 + m] if r is not None else None)
+        assert torch.equal(some, whole[1000:1000 + m]), m
+    small, x, sx, r = _case(22, 700, 4096, 70, dtype, act, form == "gated", residual=form == "residual")     # (few channels: a reduction in parts)
+    whole = small(x, sx, r)
+    forms.add("few" if "split 1," not in small.describe(40) else "")
+    some = small(x[300:340], sx[300:340].clone(), r[300:340] if r is not None else None)
+    assert torch.equal(some, whole[300:340]) and {"stream", "few"} <= forms
+    B.iconv_check(stream())
