@@ -240,12 +240,12 @@ __device__ __forceinline__ float finish_row(const RmsArgs &a, const RowSums &m, 
     const bool empty = m.top < TINY_ROW;
     float scale = m.top * (1.0f / 127.0f);
     if (!far_decides(a, m)) {
-        if (a.norm) scale *= 1.0f / sqrtf(fmaf(m.sq, a.inv_width, a.eps));
+        if (a.norm) scale *= 0.5f * (1.0f / sqrtf(fmaf(0.25f * m.sq, a.inv_width, 0.25f * a.eps)));       // (their sum may not fit either)
     } else if (m.sq < LITTLE) {
         const float root = sqrtf(fmaf(far, a.inv_width, a.eps * UP * UP));
         scale = scale < 1.0f ? scale * UP / root : scale / root * UP;
     } else {
-        scale /= fminf(sqrtf(far * a.inv_width) * (1.0f / DOWN), FLT_MAX);     // (eps is nothing here; the root itself is a float)
+        scale /= fminf(sqrtf(fmaf(far, a.inv_width, a.eps * DOWN * DOWN)) * (1.0f / DOWN), FLT_MAX);     // (the root itself is a float)
     }
     if (stores) a.scales[row] = broken ? __int_as_float(0x7fffffff) : empty ? 0.0f : scale;
     return broken || empty ? 0.0f : __fdiv_rn(127.0f, m.top);

@@ -322,3 +322,23 @@ def test_far_rows_of_every_kind(m, d, step):
 def test_very_many_rows():
     x, r, g = _data(5, (1 << 25) + 1, 3, "bf16")
     rms_check(x, r, g, *rms_call(x, r, g))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [1, 8, 9, 64, 333, 1024, 4104, 40000, 40001])
+@pytest.mark.parametrize("eps", [1e30, 1e36, 1e38, 3e38])
+def test_large_rows_beside_a_large_eps(dtype, d, eps):
+    """Squares whose sum, or whose mean with eps, a float cannot hold, and an eps of their size."""
+    size = torch.tensor([1e15, 1e17, 3e17, 1e18, 3e18, 1e19, 1.8e19, 1e20], device="cuda")[:, None]
+    sign = torch.where(torch.rand(8, d, generator=generator(1), device="cuda") < 0.5, -1.0, 1.0)
+    x = (sign * (0.5 + 0.5 * torch.rand(8, d, generator=generator(2), device="cuda")) * size).to(TYPES[dtype])
+    for g in (None, torch.rand(d, generator=generator(3), device="cuda").to(TYPES[dtype])):
+        q, scales, total = rms_call(x, None, g, eps=eps)
+        rms_check(x, None, g, q, scales, total, eps=float(torch.tensor(eps)))
+
+
+def test_many_large_wide_rows_beside_a_large_eps():
+    m, d = 148 * 4 + 3, 8192
+    x = (torch.randn(m, d, generator=generator(1), device="cuda") * 10.0 ** torch.randint(14, 22, (m, 1), generator=generator(2), device="cuda")).bfloat16()
+    for eps in (1e36, 3e38):
+        rms_check(x, None, None, *rms_call(x, eps=eps), eps=float(torch.tensor(eps)))
