@@ -795,23 +795,30 @@ StreamKernel stream_kernel(int width, bool bare)
 }
 bool bare(const RmsArgs &a) { return !a.r && !a.g; }
 
-// Shared-memory opt-in of the current device, once; its SM count.
-int stream_opt_in(int *sms)
+// Shared-memory opt-in of the current device, once.
+int stream_opt_in()
 {
-    static std::atomic<int> count[MAX_DEVICES];
+    static std::atomic<int> done[MAX_DEVICES];
     const int dev = current_device_slot();
     if (dev < 0) { set_error("irms_quant: no current device, or its index is beyond %d", MAX_DEVICES - 1); return ICONV_ERR_UNSUPPORTED; }
-    if (!count[dev].load(std::memory_order_acquire)) {
+    if (!done[dev].load(std::memory_order_acquire)) {
         for (int width = 2048; width <= STREAM_WIDTH_MAX; width *= 2)
             for (bool b : {false, true})
                 for (StreamKernel k : {stream_kernel<float>(width, b), stream_kernel<__half>(width, b), stream_kernel<__nv_bfloat16>(width, b)})
                     ICONV_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
-        int n = 0;
-        ICONV_CUDA_TRY(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-        count[dev].store(n, std::memory_order_release);
+        done[dev].store(1, std::memory_order_release);
     }
-    *sms = count[dev].load(std::memory_order_acquire);
     return ICONV_OK;
+}
+// The current device's SM count; 0 where it cannot be had.
+int sm_count()
+{
+    static std::atomic<int> count[MAX_DEVICES];
+    const int dev = current_device_slot();
+    if (dev < 0) return 0;
+    int n = count[dev].load(std::memory_order_relaxed);
+    if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) count[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // Rows of 8 KB or more, with a residual 16 KB (there a block per row has enough in flight: 8192 rows of 4096 in bfloat16 take 38 us so, 44 as a
@@ -821,15 +828,15 @@ bool streams(const RmsArgs &a, int element)
 {
     const long long bytes = (long long)a.width * element, most = MAX_SMEM - (long long)sizeof(StreamShared);
     const bool residual = a.r != nullptr;
-    return bytes >= (residual ? 16384 : 8192) && a.width <= STREAM_WIDTH_MAX && a.rows >= 4 * 148 &&
-           std::max(3, stream_groups(a.width, bare(a))) * bytes * (residual ? 2 : 1) <= most;
+    if (bytes < (residual ? 16384 : 8192) || a.width > STREAM_WIDTH_MAX || std::max(3, stream_groups(a.width, bare(a))) * bytes * (residual ? 2 : 1) > most) return false;
+    const int sms = sm_count();
+    return sms > 0 && a.rows >= 4ll * sms;
 }
 
 template <typename T>
 int launch_stream(const RmsArgs &a, cudaStream_t stream)
 {
-    int sms = 0;
-    const int rc = stream_opt_in(&sms);
+    const int rc = stream_opt_in(), sms = sm_count();
     if (rc != ICONV_OK) return rc;
     StreamArgs s;
     s.a = a;

@@ -75,3 +75,17 @@ def test_weights_further_apart_than_any():
     with pytest.raises(B.IconvError) as e:
         B.imat_plan(n=64, k=100, out_dtype=B.BF16, weights=A, scales=A, w_stride=1 << 60)
     assert e.value.status == B.ERR_SHAPE
+
+
+def test_the_streaming_product_kernel_reads_its_tensors_by_plain_loads():
+    """It comes up early too, and reads rows, scales and residual; its weights are the plan's constants, past L1 but coherent."""
+    text = open(os.path.join(CSRC, "mat_stream.cuh")).read()
+    assert "__restrict__" not in text and not re.search(r"\.nc\b", text) and "grid_dep_wait()" in text
+    assert [m.group(1).startswith("a.row_params") for m in re.finditer(r"__ldg\((.*)", text)] == [True]
+
+
+def test_many_wide_rows_are_counted_by_the_devices_sms():
+    """No SM count stands in the rules that choose a kernel."""
+    for file in ("kernel_rms.cu", "kernel_mat.cu"):
+        text = re.sub(r"//.*", "", open(os.path.join(CSRC, file)).read())
+        assert not re.search(r"\b(148|74|132)\b", text), file
