@@ -334,15 +334,18 @@ ICONV_API int iconv_stem_forward_static(const istem_desc *desc, const void *x, c
  *     v = s * weight                           in float
  *     q = [127 * v / max|v|]                   the bracket of Eq. 4: v * (127 / max|v|) in float, then floor(. + 1/2); -127 ... 127
  *     scales[row] = max|v| / 127 / sqrt(mean(s^2) + eps)
- * q * scale stands for the normed row (the root cancels in q: rounding never depends on it).  norm = 0: the 8-bit rows alone,
+ * q * scale stands for the normed row (the root cancels in q: rounding never depends on it).  q is a function of the row alone, the same in any
+ * call; the last bits of a scale are not (the squares are added up in another order where many wide rows are, and where rows start elsewhere).  norm = 0: the 8-bit rows alone,
  * scales[row] = max|v| / 127.  A row whose max|v| is zero, or lies under 2^-119, has q = 0 and scale 0; one with a NaN or an infinity in
  * v has q = 0 and scale NaN.
  *   x, residual   DEVICE rows x width of dtype (ICONV_F32, ICONV_F16 or ICONV_BF16); residual NULL: none
  *   weight        DEVICE [width] of weight_dtype (dtype or ICONV_F32); NULL: ones
  *   sum           DEVICE rows x width of dtype, or NULL: not written; may be x or residual itself, at the same stride
  *   q             DEVICE int8 rows x width; scales DEVICE float [rows]
- * Addresses are aligned to their element (16-byte aligned ones, and a width and strides in multiples of 16 bytes -- 8
- * for q, 4 with ICONV_F32 -- are the fast form).  width is at most 2^24.  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
+ * Addresses are aligned to their element.  The fast form: 16-byte aligned ones, a width and strides in multiples of 16 bytes, and for q
+ * multiples of 8 (4 with ICONV_F32).  Rows of 16-bit elements that start anywhere still go in vectors (at less than half of the fast form's rate) where q's
+ * address and stride are such multiples; everything else goes element by element, 16-bit rows of an odd width with dense rows of q too.
+ * width is at most 2^24.  rows = 0 is a no-op.  Asynchronous on cuda_stream, no workspace.
  */
 typedef struct {
     int64_t rows;
@@ -359,15 +362,15 @@ ICONV_API int irms_quant(const irms_desc *desc, const void *x, const void *resid
  * imat_plan / imat_forward -- 8-bit rows times int8 weights (int32 sums on the tensor cores, exact), with everything behind the sums in
  * the same kernel:
  *     acc[m][c] = sum_k x[m][k] * weights[c][k]
- *     y = act(acc * x_scales[m] * scales[c] + bias[c])
+ *     y = act(acc * scales[c] * x_scales[m] + bias[c])
  *     out[m][c] = y + residual[m][c]                            rounded to out_dtype (float until then)
  * and, with up_weights, both projections of a gated feed-forward block in one kernel:
- *     out[m][c] = act(gate) * up,   gate = acc * x_scales[m] * scales[c] + bias[c],   up = the same of up_weights, up_scales, up_bias
+ *     out[m][c] = act(gate) * up,   gate = acc * scales[c] * x_scales[m] + bias[c],   up = the same of up_weights, up_scales, up_bias
  * With irms_quant before them these make the sublayer: norm -> gated product -> 8-bit rows -> product with the residual.
  *
  * imat_plan copies the weights into a layout of its own, n * k bytes (twice that when gated) rounded up to blocks of 128 x 128, with
  * cudaMalloc on the current device; what desc points to may go afterwards.  It enqueues on cuda_stream and waits for it: call it outside any
- * stream capture (inside one it is refused), on the stream that wrote the weights.  ICONV_ERR_OVERFLOW when k reaches 131072 (the sums would not fit
+ * stream capture (on a stream that captures it is refused), imat_plan_destroy too, on the stream that wrote the weights.  ICONV_ERR_OVERFLOW when k reaches 131072 (the sums would not fit
  * int32 whatever the values).
  * imat_forward: a plan belongs to its device, which must be current.  It enqueues one kernel, needs no workspace and keeps nothing: calls of
  * one plan may overlap on any streams and may be captured.
@@ -378,6 +381,8 @@ ICONV_API int irms_quant(const irms_desc *desc, const void *x, const void *resid
  *   out        DEVICE rows x n of out_dtype; out and residual are aligned to their element
  * Results do not depend on the number of rows in the call.  NaN and infinities in the scales, the bias and the residual come out as the
  * formula gives them.  rows = 0 is a no-op; at most 2^30 rows.
+ * The smooth activations, besides the error of their argument: float results are off by 5e-7 of the value (an exponential's argument adds 6e-8 of itself for GELU, 2.4e-7 for
+ * tanh-GELU), 16-bit ones by 2e-6 of it before they are rounded (argument: 3e-7); a value that is y times less than 2^-126 may come out as zero in 16 bits.
  */
 typedef enum {
     IMAT_NONE = 0,

@@ -130,8 +130,9 @@ MatChoice choice_stream(const imat_plan_t *p, long long rows)
 // 110 drawn sizes its choice took 3 % longer than the best of all forms on average (geometric mean), 33 % at most.
 constexpr double SM_RATE = 87.0, HBM_RATE = 6300.0, ROUND_LATENCY = 1100.0, ISSUE = 190.0;
 
-// Up to here a few tokens stream.  The streaming kernel's blocks fill the SM's registers, so that nothing of the kernel behind comes up beside them: among
-// other kernels a call with 17 MB of weights takes 4.9 us so and 5.4 on the few-tile kernel, one with 34 MB 9.9 and 7.3, one with 67 MB 18.6 and 12.0.
+// Up to here a few tokens stream.  The streaming kernel's blocks fill the SM's registers, so that nothing of the kernel behind comes up beside them.  Whole sublayers of one
+// token, 4096 wide, whose second product has 12 / 17 / 20 / 24 / 28 / 34 / 64 MB of weights: 13.0 / 16.3 / 18.5 / 21.3 / 22.7 / 26.5 / 42.3 us with it on this kernel, 13.4 / 17.3 /
+// 18.8 / 20.8 / 22.0 / 24.8 / 40.3 on the few-tile kernel; of sixteen tokens 14.0 / 17.5 / 19.9 / 22.8 / 24.3 / 28.3 / 46.0 and 15.4 / 18.6 / 19.9 / 22.0 / 23.3 / 25.8 / 41.4.
 constexpr double MAT_STREAM_BYTES = 24.0 * 1048576.0;
 
 struct CallShape {

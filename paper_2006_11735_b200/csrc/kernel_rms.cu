@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) rms_quant_kernel(const 
 }
 
 // ---- Rows of 16-bit elements that start anywhere (an odd width without padding): vectors of 16 bytes all the same (2000 rows of 16001 with a
-// residual: 86 us, 367 element by element; 8192 of 4001 alone 46 and 80; in float single elements are as fast: 4000 of 1501 18 us, 20 so, 2000 of 8191 54 and 54).  A thread's VE
+// residual: 86 us, 367 element by element, floor 34; 8192 of 4001 alone 46 and 80, floor 15; in float single elements are as fast: 4000 of 1501 18 us, 20 so, 2000 of 8191 54 and 54).  A thread's VE
 // elements lie across two aligned 16-byte words; both are loaded (the second is the neighbour's first, and in L1) and shifted by the row's phase,
 // which is the same for all its threads.  The sum goes back the other way: a lane stores the aligned word that its own elements and the
 // lane's before it make up, and the ends of a warp's stretch go out element by element.  q's rows are aligned.
@@ -589,7 +589,7 @@ cudaError_t launch_shift(const ShiftArgs &s, cudaStream_t stream)
 }
 
 // Many wide rows: one block per SM, whose loading warps keep a ring of whole rows in shared memory ahead of the arithmetic, so that the memory
-// stays busy while a row is being reduced (a block per row has nothing in flight then: 4096 rows of 16384 in bfloat16 took 86 us, 46 this
+// stays busy while a row is being reduced (a block per row has nothing in flight then: 4096 rows of 16384 in bfloat16 took 86 us, 41 this
 // way, floor 31).  Groups of GW warps take the rows in turn, ELEMS elements a thread; a group meets at one named barrier per row.  The ring's stages
 // are a multiple of the groups, so that a stage always holds rows of one group, which has taken the one before when it waits for the next (the
 // loads may complete in any order, and a parity cannot tell two rows apart).
@@ -779,7 +779,7 @@ cudaError_t launch_width(const RmsArgs &a, cudaStream_t stream)
 using StreamKernel = void (*)(StreamArgs);
 
 // Groups that a block's warps make for rows of a width: eight of two warps, four or two, 32 elements a thread.  The widest rows: one group, unless
-// nothing but the row is read (`bare`); then the arithmetic is the bound and two groups of 64 elements a thread take turns (4096 rows of 16384: 42 us,
+// nothing but the row is read (`bare`); then the arithmetic is the bound and two groups of 64 elements a thread take turns (4096 rows of 16384: 41 us,
 // 58 in one group; with a residual and weights 1500 rows of 12000 take 28 us in one group, 36 in two).
 constexpr int STREAM_WIDTH_MAX = 8 * 32 * 64;
 int stream_groups(int width, bool bare) { return width <= 2 * 32 * 32 ? 8 : width <= 4 * 32 * 32 ? 4 : width <= 8 * 32 * 32 || bare ? 2 : 1; }
